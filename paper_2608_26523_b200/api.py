@@ -23,7 +23,10 @@ EXPORTS = ["vpp_chunk_attn_workspace_size", "vpp_chunk_attn_fwd", "vpp_lse_merge
            "vpp_static_last_error", "vpp_kv_append", "vpp_sparse_attn_workspace_size", "vpp_sparse_mla_fwd",
            "vpp_chunk_attn_partial_fwd", "vpp_tensor_map_cache_stats", "vpp_test_tensor_map_cache",
            "vpp_test_bounded_wait", "vpp_chunk_attn_host_workspace_size", "vpp_chunk_attn_host_plan",
-           "vpp_chunk_attn_host_fwd", "vpp_host_last_error"]
+           "vpp_chunk_attn_host_fwd", "vpp_host_last_error", "vpp_rope", "vpp_kv_append_rope", "vpp_block_means",
+           "vpp_block_select_workspace_size", "vpp_block_select"]
+
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
 
 
 class VppError(RuntimeError):
@@ -83,6 +86,50 @@ class HostChunkAttnArgs(ctypes.Structure):
     ]
 
 
+class RopeSpec(ctypes.Structure):
+    _fields_ = [("inv_freq", ctypes.c_void_p), ("rot_dim", ctypes.c_int32), ("rot_offset", ctypes.c_int32),
+                ("layout", ctypes.c_int32), ("amplitude", ctypes.c_float)]
+
+
+class RopeArgs(ctypes.Structure):
+    _fields_ = [
+        ("x", ctypes.c_void_p), ("out", ctypes.c_void_p), ("x_token_stride", ctypes.c_int64), ("x_head_stride", ctypes.c_int64),
+        ("out_token_stride", ctypes.c_int64), ("out_head_stride", ctypes.c_int64),
+        ("prefix_len", ctypes.c_void_p), ("chunk_len", ctypes.c_void_p), ("num_reqs", ctypes.c_int32), ("total_q", ctypes.c_int32),
+        ("num_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("rope", RopeSpec), ("status", ctypes.c_void_p),
+    ]
+
+
+class KvAppendRopeArgs(ctypes.Structure):
+    _fields_ = [
+        ("append", KvAppendArgs), ("k_new_token_stride", ctypes.c_int64), ("k_new_head_stride", ctypes.c_int64),
+        ("v_new_token_stride", ctypes.c_int64), ("v_new_head_stride", ctypes.c_int64), ("q", ctypes.c_void_p), ("q_out", ctypes.c_void_p),
+        ("q_token_stride", ctypes.c_int64), ("q_head_stride", ctypes.c_int64), ("q_out_token_stride", ctypes.c_int64),
+        ("q_out_head_stride", ctypes.c_int64), ("num_q_heads", ctypes.c_int32), ("rope", RopeSpec),
+    ]
+
+
+class BlockMeansArgs(ctypes.Structure):
+    _fields_ = [
+        ("k_cache", ctypes.c_void_p), ("k_block_stride", ctypes.c_int64), ("k_token_stride", ctypes.c_int64), ("k_head_stride", ctypes.c_int64),
+        ("k_means", ctypes.c_void_p), ("block_table", ctypes.c_void_p), ("prefix_len", ctypes.c_void_p), ("chunk_len", ctypes.c_void_p),
+        ("num_reqs", ctypes.c_int32), ("max_blocks_per_req", ctypes.c_int32), ("block_size", ctypes.c_int32),
+        ("num_blocks", ctypes.c_int32), ("total_q", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+        ("status", ctypes.c_void_p),
+    ]
+
+
+class BlockSelectArgs(ctypes.Structure):
+    _fields_ = [
+        ("q", ctypes.c_void_p), ("k_means", ctypes.c_void_p), ("block_table", ctypes.c_void_p), ("prefix_len", ctypes.c_void_p),
+        ("chunk_len", ctypes.c_void_p), ("num_reqs", ctypes.c_int32), ("max_blocks_per_req", ctypes.c_int32), ("block_size", ctypes.c_int32),
+        ("num_blocks", ctypes.c_int32), ("total_q", ctypes.c_int32), ("max_seq_len", ctypes.c_int32), ("num_q_heads", ctypes.c_int32),
+        ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("topk", ctypes.c_int32), ("num_first", ctypes.c_int32),
+        ("num_last", ctypes.c_int32), ("indices", ctypes.c_void_p), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+        ("status", ctypes.c_void_p),
+    ]
+
+
 _lib = None
 
 
@@ -131,6 +178,16 @@ def load_library():
         lib.vpp_chunk_attn_host_fwd.restype = ctypes.c_int
         lib.vpp_chunk_attn_host_fwd.argtypes = [ctypes.POINTER(HostChunkAttnArgs), ctypes.c_void_p]
         lib.vpp_host_last_error.restype = ctypes.c_char_p
+        lib.vpp_rope.restype = ctypes.c_int
+        lib.vpp_rope.argtypes = [ctypes.POINTER(RopeArgs), ctypes.c_void_p]
+        lib.vpp_kv_append_rope.restype = ctypes.c_int
+        lib.vpp_kv_append_rope.argtypes = [ctypes.POINTER(KvAppendRopeArgs), ctypes.c_void_p]
+        lib.vpp_block_means.restype = ctypes.c_int
+        lib.vpp_block_means.argtypes = [ctypes.POINTER(BlockMeansArgs), ctypes.c_void_p]
+        lib.vpp_block_select_workspace_size.restype = ctypes.c_size_t
+        lib.vpp_block_select_workspace_size.argtypes = [ctypes.POINTER(BlockSelectArgs)]
+        lib.vpp_block_select.restype = ctypes.c_int
+        lib.vpp_block_select.argtypes = [ctypes.POINTER(BlockSelectArgs), ctypes.c_void_p]
         _lib = lib
     return _lib
 
@@ -274,6 +331,86 @@ def vpp_kv_append(k_new, v_new, k_cache, v_cache, block_table, prefix_len, chunk
     if stream is None:
         stream = _current_stream()
     _check(load_library().vpp_kv_append(ctypes.byref(a), stream))
+
+
+def vpp_rope(x, out, prefix_len, chunk_len, inv_freq, layout="half", rot_offset=0, amplitude=1.0, status=None, stream=None):
+    """out <- x with features rot_offset .. rot_offset + 2 * len(inv_freq) of every head rotated to the row's position.
+
+    x, out [T, H, D] bf16, any strides with a contiguous last dim (out may be x); inv_freq fp32 [rot_dim / 2]; layout "half"
+    (feature j with j + rot_dim / 2) or "interleaved" (2 j with 2 j + 1)."""
+    assert x.shape == out.shape and x.dtype == out.dtype == torch.bfloat16 and x.stride(2) == 1 and out.stride(2) == 1
+    assert inv_freq.dtype == torch.float32 and inv_freq.is_contiguous()
+    a = RopeArgs(x.data_ptr(), out.data_ptr(), x.stride(0), x.stride(1), out.stride(0), out.stride(1), prefix_len.data_ptr(),
+                 chunk_len.data_ptr(), prefix_len.numel(), x.shape[0], x.shape[1], x.shape[2],
+                 RopeSpec(inv_freq.data_ptr(), 2 * inv_freq.numel(), int(rot_offset), ROPE_LAYOUTS[layout], float(amplitude)),
+                 None if status is None else status.data_ptr())
+    if stream is None:
+        stream = _current_stream()
+    _check(load_library().vpp_rope(ctypes.byref(a), stream))
+
+
+def vpp_kv_append_rope(k_new, v_new, k_cache, v_cache, block_table, prefix_len, chunk_len, block_size, max_seq_len, inv_freq, q=None,
+                       q_out=None, layout="half", rot_offset=0, amplitude=1.0, status=None, stream=None):
+    """vpp_kv_append with the keys rotated to their positions on the way, and q [T, Hq, Dqk] rotated into q_out (both or neither).
+
+    k_new, v_new, q, q_out: any strides with a contiguous last dim, as slices of a fused projection have them."""
+    ks, vs = k_cache.stride(), v_cache.stride() if v_cache is not None else (0, 0, 0, 1)
+    assert ks[3] == 1 and vs[3] == 1 and k_new.stride(2) == 1 and (v_new is None or v_new.stride(2) == 1)
+    assert all(t is None or t.dtype == torch.bfloat16 for t in (k_new, v_new, q, q_out, k_cache, v_cache))
+    assert inv_freq.dtype == torch.float32 and inv_freq.is_contiguous()
+    assert (q is None) == (q_out is None)
+    assert q is None or (q.shape == q_out.shape and q.stride(2) == 1 and q_out.stride(2) == 1 and q.shape[0] == k_new.shape[0] and q.shape[2] == k_new.shape[2])
+    head_dim_v = v_new.shape[2] if v_new is not None else (v_cache.shape[3] if v_cache is not None else k_new.shape[2])
+    append = KvAppendArgs(
+        k_new.data_ptr(), None if v_new is None else v_new.data_ptr(), k_cache.data_ptr(),
+        None if v_cache is None else v_cache.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2],
+        None if block_table is None else block_table.data_ptr(), prefix_len.data_ptr(), chunk_len.data_ptr(),
+        prefix_len.numel(), 0 if block_table is None else block_table.shape[1], int(block_size), k_cache.shape[0],
+        k_new.shape[0], int(max_seq_len), k_new.shape[1], k_new.shape[2], head_dim_v, None if status is None else status.data_ptr())
+    n_s, v_s = k_new.stride(), v_new.stride() if v_new is not None else (0, 0)
+    q_s, o_s = (q.stride(), q_out.stride()) if q is not None else ((0, 0), (0, 0))
+    a = KvAppendRopeArgs(append, n_s[0], n_s[1], v_s[0], v_s[1], None if q is None else q.data_ptr(),
+                         None if q is None else q_out.data_ptr(), q_s[0], q_s[1], o_s[0], o_s[1], 0 if q is None else q.shape[1],
+                         RopeSpec(inv_freq.data_ptr(), 2 * inv_freq.numel(), int(rot_offset), ROPE_LAYOUTS[layout], float(amplitude)))
+    if stream is None:
+        stream = _current_stream()
+    _check(load_library().vpp_kv_append_rope(ctypes.byref(a), stream))
+
+
+def vpp_block_means(k_cache, k_means, block_table, prefix_len, chunk_len, block_size, total_q, status=None, stream=None):
+    """k_means[page] <- mean key of every page that the chunk completes.  k_cache [num_blocks, block_size, Hkv, 128], any strides with a
+    contiguous last dim; k_means [num_blocks, Hkv, 128] bf16, dense."""
+    ks = k_cache.stride()
+    assert ks[3] == 1 and k_means.is_contiguous() and k_cache.dtype == k_means.dtype == torch.bfloat16
+    assert k_means.shape == (k_cache.shape[0], k_cache.shape[2], k_cache.shape[3])
+    a = BlockMeansArgs(k_cache.data_ptr(), ks[0], ks[1], ks[2], k_means.data_ptr(), _ptr(block_table), prefix_len.data_ptr(), chunk_len.data_ptr(),
+                       prefix_len.numel(), 0 if block_table is None else block_table.shape[1], int(block_size), k_cache.shape[0], int(total_q),
+                       k_cache.shape[2], k_cache.shape[3], None if status is None else status.data_ptr())
+    if stream is None:
+        stream = _current_stream()
+    _check(load_library().vpp_block_means(ctypes.byref(a), stream))
+
+
+def vpp_block_select_workspace_size(total_q, num_reqs, num_q_heads, num_kv_heads, block_size, max_seq_len):
+    a = BlockSelectArgs(num_reqs=int(num_reqs), block_size=int(block_size), total_q=int(total_q), max_seq_len=int(max_seq_len),
+                        num_q_heads=int(num_q_heads), num_kv_heads=int(num_kv_heads), head_dim=128, topk=1, num_last=1)
+    return int(load_library().vpp_block_select_workspace_size(ctypes.byref(a)))
+
+
+def vpp_block_select(q, k_means, block_table, prefix_len, chunk_len, block_size, max_seq_len, indices, workspace, num_first=0, num_last=1,
+                     status=None, stream=None):
+    """indices [T, Hkv, topk] int32 <- the pages that each token's queries score highest (see include/vpp.h).  q [T, Hq, 128] bf16 dense,
+    k_means [num_blocks, Hkv, 128]; workspace of vpp_block_select_workspace_size(...) bytes."""
+    assert q.is_contiguous() and k_means.is_contiguous() and indices.is_contiguous() and indices.dtype == torch.int32
+    assert indices.shape[:2] == (q.shape[0], k_means.shape[1]) and q.dtype == k_means.dtype == torch.bfloat16 and q.shape[2] == k_means.shape[2]
+    a = BlockSelectArgs(q.data_ptr(), k_means.data_ptr(), _ptr(block_table), prefix_len.data_ptr(), chunk_len.data_ptr(),
+                        prefix_len.numel(), 0 if block_table is None else block_table.shape[1], int(block_size), k_means.shape[0], q.shape[0],
+                        int(max_seq_len), q.shape[1], k_means.shape[1], q.shape[2], indices.shape[2], int(num_first), int(num_last),
+                        indices.data_ptr(), _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
+                        None if status is None else status.data_ptr())
+    if stream is None:
+        stream = _current_stream()
+    _check(load_library().vpp_block_select(ctypes.byref(a), stream))
 
 
 def vpp_sparse_attn_workspace_size(total_q):

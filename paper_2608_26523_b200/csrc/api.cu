@@ -17,13 +17,14 @@
 #include "attn_ws.cuh"
 #include "bounded.h"
 #include "common.cuh"
+#include "host.h"
 #include "kv_append.cuh"
 #include "merge.cuh"
 #include "prep.cuh"
 #include "wait_test.cuh"
 
-namespace {
-
+namespace vpp {
+namespace host {
 thread_local char g_err[512] = "";
 thread_local int32_t g_launches = 0;
 
@@ -35,31 +36,18 @@ vpp_status fail(vpp_status s, const char* fmt, ...) {
     return s;
 }
 
-size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
-
 // The status word of a call that launches nothing.
 vpp_status zero_status(int32_t* status, cudaStream_t stream) {
     if (status && cudaMemsetAsync(status, 0, sizeof(int32_t), stream) != cudaSuccess)
         return fail(VPP_ERR_CUDA, "memset status: %s", cudaGetErrorString(cudaGetLastError()));
     return VPP_OK;
 }
+}  // namespace host
+}  // namespace vpp
 
-// Launch with programmatic stream serialization: the kernel may start (and set itself up) while its predecessor in the
-// stream still runs, and waits for it (griddepcontrol.wait) before it touches memory.
-template <typename... Params, typename... Args>
-cudaError_t launch(void (*kernel)(Params...), unsigned blocks, unsigned threads, size_t smem, cudaStream_t stream, Args... args) {
-    cudaLaunchAttribute attr{};
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr.val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(blocks);
-    cfg.blockDim = dim3(threads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = stream;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...);
-}
+using namespace vpp::host;
+
+namespace {
 
 // ---- device facts, cached per device -------------------------------------------------------------
 struct DeviceInfo {
@@ -70,7 +58,9 @@ struct DeviceInfo {
 std::mutex g_mu;
 DeviceInfo g_dev[64];
 
-int sm_count_or_default() {
+}  // namespace
+
+int vpp::host::sm_count_or_default() {
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) {
         cudaGetLastError();
@@ -89,6 +79,7 @@ int sm_count_or_default() {
     return g_dev[dev].sm_count;
 }
 
+namespace {
 // ---- tensor maps ------------------------------------------------------------------------------------
 using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
                               const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
@@ -210,7 +201,9 @@ TmapKey make_key(const void* base, int rank, const uint64_t* dims, const uint64_
     return k;
 }
 
-bool make_tmap(CUtensorMap* m, const void* base, int rank, const uint64_t* dims, const uint64_t* strides_bytes,
+}  // namespace
+
+bool vpp::host::make_tmap(CUtensorMap* m, const void* base, int rank, const uint64_t* dims, const uint64_t* strides_bytes,
                const uint32_t* box) {
     return g_tmaps.get(make_key(base, rank, dims, strides_bytes, box), encode_with_driver, m);
 }
@@ -218,7 +211,7 @@ bool make_tmap(CUtensorMap* m, const void* base, int rank, const uint64_t* dims,
 // The two maps of a K or V cache of the d = 128 kernel (attn_ws.cuh) and how (block, kv-head) becomes one coordinate of the
 // first: both strides are whole numbers of `unit`.  Where that coordinate would not fit an int32 (strides with hardly a common
 // divisor in a huge cache) every tile takes the exact map.
-bool make_kv_maps(const void* base, int64_t block_stride, int64_t token_stride, int64_t head_stride, int B, int n_blocks, int heads, int box_rows,
+bool vpp::host::make_kv_maps(const void* base, int64_t block_stride, int64_t token_stride, int64_t head_stride, int B, int n_blocks, int heads, int box_rows,
                   CUtensorMap* tm, CUtensorMap* tm_exact, int32_t* block_units, int32_t* head_units, int32_t* end, int32_t* exact_from) {
     const uint64_t dx[5] = {64, static_cast<uint64_t>(B), 2, static_cast<uint64_t>(heads), static_cast<uint64_t>(n_blocks)};
     const uint64_t sx[4] = {static_cast<uint64_t>(token_stride) * 2, 128, static_cast<uint64_t>(head_stride) * 2,
@@ -243,14 +236,8 @@ bool make_kv_maps(const void* base, int64_t block_stride, int64_t token_stride, 
     return make_tmap(tm, base, 5, d, s, b);
 }
 
+namespace {
 // ---- validation -------------------------------------------------------------------------------------
-bool is_pow2(int x) { return x > 0 && (x & (x - 1)) == 0; }
-int ilog2(int x) {
-    int s = 0;
-    while ((1 << s) < x) ++s;
-    return s;
-}
-
 enum class Family { kGqa128, kMla576, kNone };
 
 vpp_status validate(const vpp_chunk_attn_args* a, Family* fam) {
@@ -866,7 +853,7 @@ vpp_status vpp_kv_append(const vpp_kv_append_args* a, vpp_stream_t stream_) {
     if (a->num_reqs < 0 || a->total_q < 0 || a->num_kv_heads <= 0 || a->head_dim_qk <= 0 || a->head_dim_v <= 0)
         return fail(VPP_ERR_INVALID_ARG, "num_reqs, total_q >= 0 and num_kv_heads, head dims > 0 required");
     if (a->head_dim_qk % 8 || a->head_dim_v % 8) return fail(VPP_ERR_UNSUPPORTED, "head dims must be multiples of 8");
-    if (a->num_reqs > vpp::kAppendMaxReqs) return fail(VPP_ERR_UNSUPPORTED, "at most %d requests", vpp::kAppendMaxReqs);
+    if (a->num_reqs > vpp::kLengthsMaxReqs) return fail(VPP_ERR_UNSUPPORTED, "at most %d requests", vpp::kLengthsMaxReqs);
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     if (a->total_q == 0 || a->num_reqs == 0) return zero_status(a->status, stream);
     if (!a->k_new || !a->k_cache || !a->prefix_len || !a->chunk_len)

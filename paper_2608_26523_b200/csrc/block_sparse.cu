@@ -1,0 +1,340 @@
+// Host side of the rotary and block-sparse entry points of include/vpp.h: argument checks and launches.
+#include <cuda_runtime.h>
+
+#include <cmath>
+#include <cstdint>
+
+#include "../../include/vpp.h"
+#include "block_means.cuh"
+#include "block_select.cuh"
+#include "common.cuh"
+#include "host.h"
+#include "lengths.cuh"
+#include "rope.cuh"
+
+using namespace vpp::host;
+
+namespace {
+
+bool mis16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
+
+vpp_status check_rope(const vpp_rope_spec& r, int head_dim) {
+    if (!r.inv_freq) return fail(VPP_ERR_INVALID_ARG, "inv_freq is null");
+    if (r.layout != VPP_ROPE_HALF && r.layout != VPP_ROPE_INTERLEAVED) return fail(VPP_ERR_INVALID_ARG, "layout must be VPP_ROPE_HALF or VPP_ROPE_INTERLEAVED");
+    if (!std::isfinite(r.amplitude)) return fail(VPP_ERR_INVALID_ARG, "amplitude must be finite");
+    if (r.rot_dim <= 0 || r.rot_dim % 16 || r.rot_dim > 2 * vpp::kRopeMaxPairs)
+        return fail(VPP_ERR_UNSUPPORTED, "rot_dim must be a multiple of 16 in 16..%d", 2 * vpp::kRopeMaxPairs);
+    if (r.rot_offset < 0 || r.rot_offset % 8) return fail(VPP_ERR_UNSUPPORTED, "rot_offset must be a non-negative multiple of 8");
+    if (r.rot_offset > head_dim - r.rot_dim) return fail(VPP_ERR_INVALID_ARG, "rot_offset + rot_dim exceeds the head dim (%d)", head_dim);
+    return VPP_OK;
+}
+
+bool good_stride(int64_t s) { return s >= 0 && s % 8 == 0; }
+
+// One launch of the rotation; p's rows, lengths and table are filled in.
+vpp_status launch_rope(vpp::RopeParams& p, const vpp_rope_spec& r, cudaStream_t stream) {
+    p.inv_freq = r.inv_freq;
+    p.pairs = r.rot_dim / 2;
+    p.first_vec = r.rot_offset / 8;
+    p.amplitude = r.amplitude;
+    const int units = p.q.units + p.k.units + p.v.units, warps = vpp::kRopeThreads / 32;
+    const long long tasks = static_cast<long long>(p.total_q) * ((units + vpp::kRopePiece - 1) / vpp::kRopePiece);
+    long long blocks = (tasks + warps - 1) / warps;
+    const long long cap = 16ll * sm_count_or_default();
+    if (blocks > cap) blocks = cap;
+    const int work_blocks = static_cast<int>(blocks);
+    auto kern = r.layout == VPP_ROPE_INTERLEAVED ? vpp::rope_kernel<true> : vpp::rope_kernel<false>;
+    const cudaError_t ce = launch(kern, static_cast<unsigned>(work_blocks + (p.status ? 1 : 0)), vpp::kRopeThreads,
+                                  sizeof(int32_t) * (static_cast<size_t>(p.num_reqs) + 1), stream, p, work_blocks);
+    if (ce != cudaSuccess) return fail(VPP_ERR_CUDA, "rotation launch: %s", cudaGetErrorString(ce));
+    return VPP_OK;
+}
+
+vpp::RopeRows rows_of(const void* src, int64_t src_token, int64_t src_head, void* dst, int64_t dst_block, int64_t dst_token, int64_t dst_head, int heads, int dim) {
+    vpp::RopeRows w{};
+    w.src = static_cast<const uint8_t*>(src);
+    w.src_token = src_token * 2;
+    w.src_head = src_head * 2;
+    w.dst = static_cast<uint8_t*>(dst);
+    w.dst_block = dst_block * 2;
+    w.dst_token = dst_token * 2;
+    w.dst_head = dst_head * 2;
+    w.per_head = dim / 16;
+    w.units = heads * w.per_head;
+    return w;
+}
+
+// Positions a request's pages can hold, as far as positions are counted (0: bad arguments).
+long long paged_capacity(int max_blocks_per_req, int block_size) {
+    const long long n = static_cast<long long>(max_blocks_per_req) * block_size;
+    return n < INT32_MAX ? n : INT32_MAX;
+}
+
+vpp_status check_paged(const int32_t* block_table, int block_size, int max_blocks_per_req, int num_blocks) {
+    if (!block_table) return fail(VPP_ERR_UNSUPPORTED, "a block table is required: pages are the blocks");
+    if (!is_pow2(block_size)) return fail(VPP_ERR_UNSUPPORTED, "block_size must be a power of two");
+    if (max_blocks_per_req <= 0 || num_blocks <= 0) return fail(VPP_ERR_INVALID_ARG, "max_blocks_per_req and num_blocks must be > 0");
+    return VPP_OK;
+}
+
+// ---- page selection: slabs of tokens, and where their scores are ----
+struct SelectPlan {
+    int row_pages;        // floats of a row of scores
+    int slab;             // tokens of a slab
+    int run_pages, runs;  // pages of an item, items along a row
+    int items;            // most items of a slab
+    size_t scores, bounds, bad, total;
+};
+
+vpp_status select_plan(const vpp_block_select_args* a, SelectPlan* s) {
+    if (!a) return fail(VPP_ERR_INVALID_ARG, "args is null");
+    if (a->num_reqs < 0 || a->total_q < 0 || a->max_seq_len < 0) return fail(VPP_ERR_INVALID_ARG, "num_reqs, total_q and max_seq_len must be >= 0");
+    if (a->num_q_heads <= 0 || a->num_kv_heads <= 0 || a->num_q_heads % a->num_kv_heads != 0)
+        return fail(VPP_ERR_INVALID_ARG, "num_q_heads (%d) must be a positive multiple of num_kv_heads (%d)", a->num_q_heads, a->num_kv_heads);
+    if (a->head_dim != 128 || a->num_q_heads / a->num_kv_heads > 128)
+        return fail(VPP_ERR_UNSUPPORTED, "head_dim must be 128 and groups of q-heads at most 128");
+    if (a->num_reqs > vpp::kLengthsMaxReqs) return fail(VPP_ERR_UNSUPPORTED, "at most %d requests", vpp::kLengthsMaxReqs);
+    if (!is_pow2(a->block_size)) return fail(VPP_ERR_UNSUPPORTED, "block_size must be a power of two");
+    if (a->topk < 1 || a->topk > vpp::kSelectMaxTopk) return fail(VPP_ERR_UNSUPPORTED, "topk must be in 1..%d", vpp::kSelectMaxTopk);
+    if (a->num_first < 0 || a->num_last < 1 || a->num_first > a->topk || a->num_last > a->topk - a->num_first)
+        return fail(VPP_ERR_INVALID_ARG, "need num_first >= 0, num_last >= 1 and num_first + num_last <= topk");
+    const long long T = a->total_q > 0 ? a->total_q : 1, H = a->num_kv_heads;
+    const long long pages = a->max_seq_len / a->block_size + 1;
+    s->row_pages = static_cast<int>((pages + vpp::kSelectTile - 1) / vpp::kSelectTile * vpp::kSelectTile);
+    long long slab = vpp::kSelectSlabBytes / (4ll * s->row_pages * H);
+    slab = slab / vpp::kSelectTile * vpp::kSelectTile;         // (whole tiles of a long chunk)
+    if (slab < vpp::kSelectTile) slab = vpp::kSelectTile;
+    if (slab > T) slab = T;
+    s->slab = static_cast<int>(slab);
+    // runs of pages: one where the tiles fill the SMs, else as many as give each about one item
+    const long long tiles_ub = (slab + vpp::kSelectTile - 1) / vpp::kSelectTile + a->num_reqs;
+    const long long tiles = tiles_ub < slab ? tiles_ub : slab;           // (every tile has a token)
+    const long long steps = s->row_pages / vpp::kSelectTile;
+    long long runs = (2ll * sm_count_or_default()) / (tiles * H);
+    if (runs < 1) runs = 1;
+    if (runs > steps) runs = steps;
+    s->run_pages = static_cast<int>((steps + runs - 1) / runs) * vpp::kSelectTile;
+    s->runs = (s->row_pages + s->run_pages - 1) / s->run_pages;
+    const long long items = tiles * H * s->runs;
+    if (items > INT32_MAX) return fail(VPP_ERR_UNSUPPORTED, "too many requests times heads");
+    s->items = static_cast<int>(items);
+    s->scores = 0;
+    s->bounds = align_up(s->scores + static_cast<size_t>(slab) * H * s->row_pages * 4, 256);
+    s->bad = align_up(s->bounds + static_cast<size_t>(slab) * H * s->runs * 4, 256);
+    s->total = align_up(s->bad + static_cast<size_t>(s->items) * 4, 256);
+    return VPP_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+vpp_status vpp_rope(const vpp_rope_args* a, vpp_stream_t stream_) {
+    g_err[0] = 0;
+    if (!a) return fail(VPP_ERR_INVALID_ARG, "args is null");
+    if (a->num_reqs < 0 || a->total_q < 0 || a->num_heads <= 0 || a->head_dim <= 0)
+        return fail(VPP_ERR_INVALID_ARG, "num_reqs, total_q >= 0 and num_heads, head_dim > 0 required");
+    if (a->head_dim % 16) return fail(VPP_ERR_UNSUPPORTED, "head_dim must be a multiple of 16");
+    if (static_cast<int64_t>(a->num_heads) * a->head_dim > INT32_MAX) return fail(VPP_ERR_UNSUPPORTED, "num_heads * head_dim exceeds 2^31 - 1");
+    if (a->num_reqs > vpp::kLengthsMaxReqs) return fail(VPP_ERR_UNSUPPORTED, "at most %d requests", vpp::kLengthsMaxReqs);
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    if (a->total_q == 0 || a->num_reqs == 0) return zero_status(a->status, stream);
+    const vpp_status st = check_rope(a->rope, a->head_dim);
+    if (st != VPP_OK) return st;
+    if (!a->x || !a->out || !a->prefix_len || !a->chunk_len) return fail(VPP_ERR_INVALID_ARG, "x, out, prefix_len and chunk_len must be non-null");
+    if (mis16(a->x) || mis16(a->out)) return fail(VPP_ERR_INVALID_ARG, "x and out must be 16-byte aligned");
+    if (!good_stride(a->x_token_stride) || !good_stride(a->x_head_stride) || !good_stride(a->out_token_stride) || !good_stride(a->out_head_stride))
+        return fail(VPP_ERR_INVALID_ARG, "strides must be non-negative multiples of 8 elements");
+    vpp::RopeParams p{};
+    p.q = rows_of(a->x, a->x_token_stride, a->x_head_stride, a->out, 0, a->out_token_stride, a->out_head_stride, a->num_heads, a->head_dim);
+    p.prefix_len = a->prefix_len;
+    p.chunk_len = a->chunk_len;
+    p.num_reqs = a->num_reqs;
+    p.capacity = INT32_MAX;
+    p.total_q = a->total_q;
+    p.status = a->status;
+    p.k.per_head = p.v.per_head = 1;
+    return launch_rope(p, a->rope, stream);
+}
+
+vpp_status vpp_kv_append_rope(const vpp_kv_append_rope_args* args, vpp_stream_t stream_) {
+    g_err[0] = 0;
+    if (!args) return fail(VPP_ERR_INVALID_ARG, "args is null");
+    const vpp_kv_append_args* a = &args->append;
+    if (a->num_reqs < 0 || a->total_q < 0 || a->num_kv_heads <= 0 || a->head_dim_qk <= 0 || a->head_dim_v <= 0)
+        return fail(VPP_ERR_INVALID_ARG, "num_reqs, total_q >= 0 and num_kv_heads, head dims > 0 required");
+    if (a->head_dim_qk % 16 || a->head_dim_v % 16) return fail(VPP_ERR_UNSUPPORTED, "head dims must be multiples of 16");
+    if ((args->q == nullptr) != (args->q_out == nullptr)) return fail(VPP_ERR_INVALID_ARG, "q and q_out go together");
+    if (args->q && args->num_q_heads <= 0) return fail(VPP_ERR_INVALID_ARG, "num_q_heads must be > 0 with q");
+    const int64_t heads = static_cast<int64_t>(args->q ? args->num_q_heads : 0) + a->num_kv_heads;
+    if (heads * a->head_dim_qk + static_cast<int64_t>(a->num_kv_heads) * a->head_dim_v > INT32_MAX)
+        return fail(VPP_ERR_UNSUPPORTED, "a token's heads exceed 2^31 - 1 features");
+    if (a->num_reqs > vpp::kLengthsMaxReqs) return fail(VPP_ERR_UNSUPPORTED, "at most %d requests", vpp::kLengthsMaxReqs);
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    if (a->total_q == 0 || a->num_reqs == 0) return zero_status(a->status, stream);
+    vpp_status st = check_rope(args->rope, a->head_dim_qk);
+    if (st != VPP_OK) return st;
+    if (!a->k_new || !a->k_cache || !a->prefix_len || !a->chunk_len)
+        return fail(VPP_ERR_INVALID_ARG, "k_new, k_cache, prefix_len and chunk_len must be non-null");
+    if (a->v_new && !a->v_cache) return fail(VPP_ERR_INVALID_ARG, "v_new given without v_cache");
+    vpp::RopeParams p{};
+    p.capacity = a->max_seq_len;
+    if (a->block_table) {
+        st = check_paged(a->block_table, a->block_size, a->max_blocks_per_req, a->num_blocks);
+        if (st != VPP_OK) return st;
+        p.block_shift = ilog2(a->block_size);
+        p.capacity = paged_capacity(a->max_blocks_per_req, a->block_size);
+    } else if (a->max_seq_len <= 0) {
+        return fail(VPP_ERR_INVALID_ARG, "max_seq_len must be > 0 for a contiguous cache");
+    }
+    bool good = good_stride(a->k_block_stride) && good_stride(a->k_token_stride) && good_stride(a->k_head_stride) &&
+                good_stride(args->k_new_token_stride) && good_stride(args->k_new_head_stride);
+    bool mis = mis16(a->k_new) || mis16(a->k_cache);
+    if (a->v_new) {
+        good = good && good_stride(a->v_block_stride) && good_stride(a->v_token_stride) && good_stride(a->v_head_stride) &&
+               good_stride(args->v_new_token_stride) && good_stride(args->v_new_head_stride);
+        mis = mis || mis16(a->v_new) || mis16(a->v_cache);
+    }
+    if (args->q) {
+        good = good && good_stride(args->q_token_stride) && good_stride(args->q_head_stride) && good_stride(args->q_out_token_stride) &&
+               good_stride(args->q_out_head_stride);
+        mis = mis || mis16(args->q) || mis16(args->q_out);
+    }
+    if (!good) return fail(VPP_ERR_INVALID_ARG, "strides must be non-negative multiples of 8 elements");
+    if (mis) return fail(VPP_ERR_INVALID_ARG, "k_new, v_new, q, q_out and the caches must be 16-byte aligned");
+    p.q.per_head = p.v.per_head = 1;
+    if (args->q)
+        p.q = rows_of(args->q, args->q_token_stride, args->q_head_stride, args->q_out, 0, args->q_out_token_stride, args->q_out_head_stride,
+                      args->num_q_heads, a->head_dim_qk);
+    p.k = rows_of(a->k_new, args->k_new_token_stride, args->k_new_head_stride, a->k_cache, a->k_block_stride, a->k_token_stride, a->k_head_stride,
+                  a->num_kv_heads, a->head_dim_qk);
+    if (a->v_new)
+        p.v = rows_of(a->v_new, args->v_new_token_stride, args->v_new_head_stride, a->v_cache, a->v_block_stride, a->v_token_stride, a->v_head_stride,
+                      a->num_kv_heads, a->head_dim_v);
+    p.block_table = a->block_table;
+    p.prefix_len = a->prefix_len;
+    p.chunk_len = a->chunk_len;
+    p.num_reqs = a->num_reqs;
+    p.max_blocks_per_req = a->max_blocks_per_req;
+    p.num_blocks = a->num_blocks;
+    p.total_q = a->total_q;
+    p.status = a->status;
+    return launch_rope(p, args->rope, stream);
+}
+
+vpp_status vpp_block_means(const vpp_block_means_args* a, vpp_stream_t stream_) {
+    g_err[0] = 0;
+    if (!a) return fail(VPP_ERR_INVALID_ARG, "args is null");
+    if (a->num_reqs < 0 || a->total_q < 0 || a->num_kv_heads <= 0) return fail(VPP_ERR_INVALID_ARG, "num_reqs, total_q >= 0 and num_kv_heads > 0 required");
+    if (a->head_dim != 128) return fail(VPP_ERR_UNSUPPORTED, "head_dim must be 128");
+    if (a->num_reqs > vpp::kLengthsMaxReqs) return fail(VPP_ERR_UNSUPPORTED, "at most %d requests", vpp::kLengthsMaxReqs);
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    if (a->total_q == 0 || a->num_reqs == 0) return zero_status(a->status, stream);
+    const vpp_status st = check_paged(a->block_table, a->block_size, a->max_blocks_per_req, a->num_blocks);
+    if (st != VPP_OK) return st;
+    if (!a->k_cache || !a->k_means || !a->prefix_len || !a->chunk_len)
+        return fail(VPP_ERR_INVALID_ARG, "k_cache, k_means, prefix_len and chunk_len must be non-null");
+    if (mis16(a->k_cache) || mis16(a->k_means)) return fail(VPP_ERR_INVALID_ARG, "k_cache and k_means must be 16-byte aligned");
+    if (!good_stride(a->k_block_stride) || !good_stride(a->k_token_stride) || !good_stride(a->k_head_stride))
+        return fail(VPP_ERR_INVALID_ARG, "strides must be non-negative multiples of 8 elements");
+    vpp::MeansParams p{};
+    p.k_cache = static_cast<const uint8_t*>(a->k_cache);
+    p.block_stride = a->k_block_stride * 2;
+    p.token_stride = a->k_token_stride * 2;
+    p.head_stride = a->k_head_stride * 2;
+    p.means = static_cast<uint4*>(a->k_means);
+    p.block_table = a->block_table;
+    p.prefix_len = a->prefix_len;
+    p.chunk_len = a->chunk_len;
+    p.num_reqs = a->num_reqs;
+    p.max_blocks_per_req = a->max_blocks_per_req;
+    p.block_shift = ilog2(a->block_size);
+    p.num_blocks = a->num_blocks;
+    p.capacity = paged_capacity(a->max_blocks_per_req, a->block_size);
+    p.total_q = a->total_q;
+    p.num_kv_heads = a->num_kv_heads;
+    p.status = a->status;
+    // a request completes at most one page more than its chunk fills
+    long long pages = static_cast<long long>(a->total_q) / a->block_size + a->num_reqs;
+    if (pages > a->total_q) pages = a->total_q;
+    long long blocks = pages * a->num_kv_heads;
+    const long long cap = 16ll * sm_count_or_default();
+    if (blocks > cap) blocks = cap;
+    const int work_blocks = static_cast<int>(blocks);
+    const cudaError_t ce = launch(vpp::block_means_kernel, static_cast<unsigned>(work_blocks + (a->status ? 1 : 0)), vpp::kMeansThreads,
+                                  sizeof(int32_t) * (static_cast<size_t>(a->num_reqs) + 1), stream, p, work_blocks);
+    if (ce != cudaSuccess) return fail(VPP_ERR_CUDA, "page means launch: %s", cudaGetErrorString(ce));
+    return VPP_OK;
+}
+
+size_t vpp_block_select_workspace_size(const vpp_block_select_args* a) {
+    g_err[0] = 0;
+    SelectPlan s{};
+    return select_plan(a, &s) == VPP_OK ? s.total : 0;
+}
+
+vpp_status vpp_block_select(const vpp_block_select_args* a, vpp_stream_t stream_) {
+    g_err[0] = 0;
+    SelectPlan s{};
+    vpp_status st = select_plan(a, &s);
+    if (st != VPP_OK) return st;
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    if (a->total_q == 0 || a->num_reqs == 0) return zero_status(a->status, stream);
+    st = check_paged(a->block_table, a->block_size, a->max_blocks_per_req, a->num_blocks);
+    if (st != VPP_OK) return st;
+    if (!a->q || !a->k_means || !a->prefix_len || !a->chunk_len || !a->indices)
+        return fail(VPP_ERR_INVALID_ARG, "q, k_means, prefix_len, chunk_len and indices must be non-null");
+    if (mis16(a->q) || mis16(a->k_means)) return fail(VPP_ERR_INVALID_ARG, "q and k_means must be 16-byte aligned");
+    if (!a->workspace || a->workspace_bytes < s.total) return fail(VPP_ERR_WORKSPACE, "workspace: need %zu bytes, got %zu", s.total, a->workspace_bytes);
+    if (reinterpret_cast<uintptr_t>(a->workspace) & 255u) return fail(VPP_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+    uint8_t* ws = static_cast<uint8_t*>(a->workspace);
+    vpp::SelectParams p{};
+    p.q = static_cast<const uint8_t*>(a->q);
+    p.means = static_cast<const uint8_t*>(a->k_means);
+    p.block_table = a->block_table;
+    p.prefix_len = a->prefix_len;
+    p.chunk_len = a->chunk_len;
+    p.num_reqs = a->num_reqs;
+    p.max_blocks_per_req = a->max_blocks_per_req;
+    p.block_shift = ilog2(a->block_size);
+    p.num_blocks = a->num_blocks;
+    // rows of scores are as long as max_seq_len has pages, and the table as wide as max_blocks_per_req
+    p.capacity = paged_capacity(a->max_blocks_per_req, a->block_size);
+    if (p.capacity > a->max_seq_len) p.capacity = a->max_seq_len;
+    p.total_q = a->total_q;
+    p.num_q_heads = a->num_q_heads;
+    p.num_kv_heads = a->num_kv_heads;
+    p.topk = a->topk;
+    p.num_first = a->num_first;
+    p.num_last = a->num_last;
+    p.run_pages = s.run_pages;
+    p.runs = s.runs;
+    p.row_pages = s.row_pages;
+    p.scores = reinterpret_cast<float*>(ws + s.scores);
+    p.bounds = reinterpret_cast<float*>(ws + s.bounds);
+    p.bad = reinterpret_cast<int32_t*>(ws + s.bad);
+    p.items = s.items;
+    p.indices = a->indices;
+    p.status = a->status;
+    const size_t lens = sizeof(int32_t) * (static_cast<size_t>(a->num_reqs) + 1);
+    const size_t smem_scores = vpp::kSelectSmem + 2 * lens, smem_pick = vpp::kPickSmem + lens;
+    cudaError_t ce = cudaFuncSetAttribute(vpp::block_scores_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem_scores));
+    if (ce == cudaSuccess) ce = cudaFuncSetAttribute(vpp::block_pick_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem_pick));
+    if (ce != cudaSuccess) return fail(VPP_ERR_CUDA, "page selection attributes: %s", cudaGetErrorString(ce));
+    for (int64_t row0 = 0; row0 < a->total_q; row0 += s.slab) {
+        p.row0 = static_cast<int32_t>(row0);
+        p.row1 = static_cast<int32_t>(row0 + s.slab < a->total_q ? row0 + s.slab : a->total_q);
+        ce = launch(vpp::block_scores_kernel, static_cast<unsigned>(s.items), vpp::kSelectThreads, smem_scores, stream, p);
+        if (ce != cudaSuccess) return fail(VPP_ERR_CUDA, "page scores launch: %s", cudaGetErrorString(ce));
+        const long long rows = static_cast<long long>(p.row1 - p.row0) * a->num_kv_heads, warps = vpp::kPickThreads / 32;
+        long long blocks = (rows + warps - 1) / warps;
+        const long long cap = 8ll * sm_count_or_default();
+        if (blocks > cap) blocks = cap;
+        const int work_blocks = static_cast<int>(blocks);
+        ce = launch(vpp::block_pick_kernel, static_cast<unsigned>(work_blocks + (a->status ? 1 : 0)), vpp::kPickThreads, smem_pick, stream, p, work_blocks);
+        if (ce != cudaSuccess) return fail(VPP_ERR_CUDA, "page selection launch: %s", cudaGetErrorString(ce));
+    }
+    return VPP_OK;
+}
+
+}  // extern "C"

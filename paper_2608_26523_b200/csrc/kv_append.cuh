@@ -11,6 +11,7 @@
 #pragma once
 #include <cstdint>
 
+#include "lengths.cuh"
 #include "ptx.cuh"
 
 namespace vpp {
@@ -18,7 +19,6 @@ namespace vpp {
 constexpr int kAppendThreads = 256;
 constexpr int kAppendUnroll = 8;
 constexpr int kAppendPiece = 32 * kAppendUnroll;   // 16-byte vectors a warp moves at a time
-constexpr int kAppendMaxReqs = 8192;   // the scan of chunk_len lives in shared memory (32 KB + 4)
 
 struct AppendParams {
     const uint4* k_new;      // [total_q, Hkv, Dqk] bf16 as 16-byte vectors
@@ -43,54 +43,6 @@ __device__ __forceinline__ uint4 ld_stream(const uint4* p) {
                  : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
                  : "l"(p));
     return v;
-}
-
-// Exclusive scan of chunk_len into cu[0 .. num_reqs] (shared memory); true if the lengths describe the launch.
-__device__ __forceinline__ bool append_scan(const AppendParams& p, int32_t* cu) {
-    __shared__ int s_bad;
-    const int tid = threadIdx.x, lane = tid & 31;
-    if (tid == 0) s_bad = 0;
-    __syncthreads();
-    bool bad = false;
-    for (int r = tid; r < p.num_reqs; r += kAppendThreads) {   // (all loads at once, then the scan from shared memory)
-        int c = p.chunk_len[r];
-        const int pre = p.prefix_len[r];
-        if (c < 0 || pre < 0 || static_cast<long long>(pre) + c > p.capacity) {
-            bad = true;
-            c = 0;
-        }
-        cu[r] = c;
-    }
-    if (bad) s_bad = 1;
-    __syncthreads();
-    if (tid < 32) {
-        int carry = 0;
-        for (int base = 0; base < p.num_reqs; base += 32) {
-            const int r = base + lane;
-            const int c = r < p.num_reqs ? cu[r] : 0;
-            int x = c;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int y = __shfl_up_sync(0xffffffffu, x, o);
-                if (lane >= o) x += y;
-            }
-            if (r < p.num_reqs) cu[r] = carry + x - c;
-            carry += __shfl_sync(0xffffffffu, x, 31);
-        }
-        if (lane == 0) cu[p.num_reqs] = carry;
-    }
-    __syncthreads();
-    return !s_bad && cu[p.num_reqs] == p.total_q;
-}
-
-// Request of row g (0 <= g < total_q): the last r with cu[r] <= g.
-__device__ __forceinline__ int append_request(const int32_t* cu, int num_reqs, int g) {
-    int lo = 0, hi = num_reqs - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (cu[mid] <= g) lo = mid; else hi = mid - 1;
-    }
-    return lo;
 }
 
 // The verdict on the launch (one block): lengths, and the pages of every row.  Looked up are the pages of each request's first and
@@ -123,7 +75,7 @@ __device__ __forceinline__ void append_status(const AppendParams& p, const int32
 #pragma unroll
             for (int i = 0; i < kAppendProbes; ++i) {
                 const long long g = g0 + i * kAppendThreads * step;
-                r[i] = g < p.total_q ? append_request(cu, p.num_reqs, static_cast<int>(g)) : -1;
+                r[i] = g < p.total_q ? request_of(cu, p.num_reqs, static_cast<int>(g)) : -1;
                 pos[i] = r[i] >= 0 ? __ldg(p.prefix_len + r[i]) + static_cast<int>(g - cu[r[i]]) : 0;
             }
 #pragma unroll
@@ -141,7 +93,7 @@ __global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(const AppendP
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     pdl_launch_dependents();
     pdl_wait();                       // the rows and the lengths may come from the kernel launched just before
-    const bool ok = append_scan(p, cu);
+    const bool ok = scan_lengths<kAppendThreads>(p.prefix_len, p.chunk_len, p.num_reqs, p.capacity, p.total_q, cu);
     if (static_cast<int>(blockIdx.x) >= copy_blocks) {
         append_status(p, cu, ok);
         return;
@@ -164,7 +116,7 @@ __global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(const AppendP
         long long blk = 0;
         int slot = 0;
         if (lane == 0) {
-            const int lo = append_request(cu, p.num_reqs, row);
+            const int lo = request_of(cu, p.num_reqs, row);
             const int pos = p.prefix_len[lo] + (row - cu[lo]);
             if (p.block_table == nullptr) {
                 blk = lo;
