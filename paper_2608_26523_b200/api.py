@@ -24,7 +24,7 @@ EXPORTS = ["vpp_chunk_attn_workspace_size", "vpp_chunk_attn_fwd", "vpp_lse_merge
            "vpp_chunk_attn_partial_fwd", "vpp_tensor_map_cache_stats", "vpp_test_tensor_map_cache",
            "vpp_test_bounded_wait", "vpp_chunk_attn_host_workspace_size", "vpp_chunk_attn_host_plan",
            "vpp_chunk_attn_host_fwd", "vpp_host_last_error", "vpp_rope", "vpp_kv_append_rope", "vpp_block_means",
-           "vpp_block_select_workspace_size", "vpp_block_select"]
+           "vpp_block_select_workspace_size", "vpp_block_select", "vpp_block_attn_workspace_size", "vpp_block_attn_fwd"]
 
 ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
 
@@ -188,6 +188,10 @@ def load_library():
         lib.vpp_block_select_workspace_size.argtypes = [ctypes.POINTER(BlockSelectArgs)]
         lib.vpp_block_select.restype = ctypes.c_int
         lib.vpp_block_select.argtypes = [ctypes.POINTER(BlockSelectArgs), ctypes.c_void_p]
+        lib.vpp_block_attn_workspace_size.restype = ctypes.c_size_t
+        lib.vpp_block_attn_workspace_size.argtypes = [ctypes.POINTER(ChunkAttnArgs), ctypes.c_int32]
+        lib.vpp_block_attn_fwd.restype = ctypes.c_int
+        lib.vpp_block_attn_fwd.argtypes = [ctypes.POINTER(ChunkAttnArgs), ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p]
         _lib = lib
     return _lib
 
@@ -411,6 +415,18 @@ def vpp_block_select(q, k_means, block_table, prefix_len, chunk_len, block_size,
     if stream is None:
         stream = _current_stream()
     _check(load_library().vpp_block_select(ctypes.byref(a), stream))
+
+
+def vpp_block_attn_workspace_size(args, topk):
+    return int(load_library().vpp_block_attn_workspace_size(ctypes.byref(args), int(topk)))
+
+
+def vpp_block_attn_fwd(args, indices, stream=None):
+    """Attention of the launch described by `args` (make_args) over the pages listed in indices [T, Hkv, topk] int32."""
+    assert indices.dtype == torch.int32 and indices.is_contiguous() and indices.shape[:2] == (args.total_q, args.num_kv_heads)
+    if stream is None:
+        stream = _current_stream()
+    _check(load_library().vpp_block_attn_fwd(ctypes.byref(args), indices.data_ptr(), indices.shape[2], stream))
 
 
 def vpp_sparse_attn_workspace_size(total_q):

@@ -517,6 +517,17 @@ MergeKernel pick_merge_kernel(int splits, long long total_q, int num_q_heads, in
     return vpp::lse_merge_kernel<2, 4>;
 }
 
+}  // namespace
+
+cudaError_t vpp::host::launch_merge(const float* o_parts, const float* lse_parts, int splits, int total_q, int num_q_heads, int head_dim_v,
+                                    const WorkHeader* header, void* out, float* lse, cudaStream_t stream) {
+    unsigned blocks = 1;
+    const MergeKernel mk = pick_merge_kernel(splits, total_q, num_q_heads, head_dim_v, sm_count_or_default(), &blocks);
+    return launch(mk, blocks, vpp::kMergeThreads, 0, stream, o_parts, lse_parts, splits, total_q, num_q_heads, head_dim_v, nullptr, header,
+                  static_cast<__nv_bfloat16*>(out), lse);
+}
+
+namespace {
 vpp::WorkspaceLayout layout_of(const vpp_chunk_attn_args* a, Family fam, SplitPlan plan) {
     vpp::WorkspaceLayout L{};
     const int S = plan.splits;

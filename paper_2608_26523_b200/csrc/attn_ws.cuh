@@ -75,7 +75,7 @@ struct WsItem {
 // registers):  out = (a0 O_0 + a1 O_1) / (a0 l_0 + a1 l_1),  a_t = 2^(m_t - m).  O_1 sits 128 columns after O_0.
 // (every argument by value: a reference to the kernel's parameter block or to the work unit would force them into
 // local memory for the whole kernel)
-__device__ __noinline__ void ws_packed_merge(void* out, float* lse_out, float* o_parts, float* lse_parts, bool final,
+__device__ __noinline__ inline void ws_packed_merge(void* out, float* lse_out, float* o_parts, float* lse_parts, bool final,
                                              long long out_row, bool second, const float* xm,
                                              uint32_t tO, int row, int tile_rows, float m_ref, float l_run) {
     const float m1 = xm[row], l1 = xm[128 + row];

@@ -5,6 +5,7 @@
 #include <cstdint>
 
 #include "../../include/vpp.h"
+#include "attn_blk.cuh"
 #include "block_means.cuh"
 #include "block_select.cuh"
 #include "common.cuh"
@@ -122,6 +123,64 @@ vpp_status select_plan(const vpp_block_select_args* a, SelectPlan* s) {
     s->bounds = align_up(s->scores + static_cast<size_t>(slab) * H * s->row_pages * 4, 256);
     s->bad = align_up(s->bounds + static_cast<size_t>(slab) * H * s->runs * 4, 256);
     s->total = align_up(s->bad + static_cast<size_t>(s->items) * 4, 256);
+    return VPP_OK;
+}
+
+// ---- attention over listed pages: tiles, parts and where the lists are ----
+struct BlockPlan {
+    int group, tile_tokens, words, max_tiles, max_pages, splits;
+    size_t items, pages, masks, o_parts, lse_parts, total;
+};
+constexpr int kBlockMaxTopk = 1024;
+
+vpp_status block_plan(const vpp_chunk_attn_args* a, int32_t topk, BlockPlan* b) {
+    if (!a) return fail(VPP_ERR_INVALID_ARG, "args is null");
+    if (a->num_reqs < 0 || a->total_q < 0 || a->max_seq_len < 0) return fail(VPP_ERR_INVALID_ARG, "num_reqs, total_q and max_seq_len must be >= 0");
+    if (a->num_q_heads <= 0 || a->num_kv_heads <= 0 || a->num_q_heads % a->num_kv_heads != 0)
+        return fail(VPP_ERR_INVALID_ARG, "num_q_heads (%d) must be a positive multiple of num_kv_heads (%d)", a->num_q_heads, a->num_kv_heads);
+    if (!(a->softmax_scale > 0.f) || !std::isfinite(a->softmax_scale)) return fail(VPP_ERR_INVALID_ARG, "softmax_scale must be positive and finite");
+    if (a->num_kv_splits < 0 || a->num_kv_splits > 64) return fail(VPP_ERR_INVALID_ARG, "num_kv_splits must be in [0, 64]");
+    b->group = a->num_q_heads / a->num_kv_heads;
+    if (a->head_dim_qk != 128 || a->head_dim_v != 128 || b->group > 128)
+        return fail(VPP_ERR_UNSUPPORTED, "head dims must be (128, 128) and groups of q-heads at most 128");
+    if (!is_pow2(a->block_size) || a->block_size < 16 || a->block_size > 128) return fail(VPP_ERR_UNSUPPORTED, "block_size must be 16, 32, 64 or 128");
+    if (topk < 1 || topk > kBlockMaxTopk) return fail(VPP_ERR_UNSUPPORTED, "topk must be in 1..%d", kBlockMaxTopk);
+    if (a->num_reqs > vpp::kLengthsMaxReqs) return fail(VPP_ERR_UNSUPPORTED, "at most %d requests", vpp::kLengthsMaxReqs);
+    b->tile_tokens = 128 / b->group;
+    b->words = (b->tile_tokens + 31) / 32;
+    const long long T = a->total_q, H = a->num_kv_heads;
+    long long tiles = (T + b->tile_tokens - 1) / b->tile_tokens + a->num_reqs;
+    if (tiles > T) tiles = T;                                  // (every tile has a token)
+    const long long context = (static_cast<long long>(a->max_seq_len) + a->block_size - 1) / a->block_size;
+    long long pages = static_cast<long long>(b->tile_tokens) * topk;
+    if (pages > context) pages = context;
+    if (pages < 1) pages = 1;
+    b->max_tiles = static_cast<int>(tiles);
+    b->max_pages = static_cast<int>(pages);
+    // Parts of the unions: where there are fewer tiles than SMs.
+    const int per_step = 128 / a->block_size;
+    const long long listed = T <= a->num_reqs && topk < pages ? topk : pages;      // (decode rows: a tile has one list)
+    const long long steps = (listed + per_step - 1) / per_step, work = tiles * H, sms = sm_count_or_default();
+    long long s = a->num_kv_splits;
+    if (s == 0) {
+        s = work > 0 ? sms / work : 1;
+        if (s > steps / 2) s = steps / 2;
+        if (s > 16) s = 16;
+    }
+    if (s > steps) s = steps;
+    if (s < 1) s = 1;
+    b->splits = static_cast<int>(s);
+    if (tiles * H * s > INT32_MAX) return fail(VPP_ERR_UNSUPPORTED, "too many tokens times heads");
+    const size_t lists = static_cast<size_t>(tiles * H) * pages;
+    b->items = align_up(sizeof(vpp::WorkHeader), 256);
+    b->pages = align_up(b->items + sizeof(vpp::BlkItem) * static_cast<size_t>(tiles * H), 256);
+    b->masks = align_up(b->pages + sizeof(int2) * lists, 256);
+    b->o_parts = b->lse_parts = b->total = align_up(b->masks + sizeof(uint32_t) * lists * b->words, 256);
+    if (s > 1) {
+        const size_t rows = static_cast<size_t>(s) * T * a->num_q_heads;
+        b->lse_parts = align_up(b->o_parts + rows * 128 * sizeof(float), 256);
+        b->total = align_up(b->lse_parts + rows * sizeof(float), 256);
+    }
     return VPP_OK;
 }
 
@@ -333,6 +392,116 @@ vpp_status vpp_block_select(const vpp_block_select_args* a, vpp_stream_t stream_
         const int work_blocks = static_cast<int>(blocks);
         ce = launch(vpp::block_pick_kernel, static_cast<unsigned>(work_blocks + (a->status ? 1 : 0)), vpp::kPickThreads, smem_pick, stream, p, work_blocks);
         if (ce != cudaSuccess) return fail(VPP_ERR_CUDA, "page selection launch: %s", cudaGetErrorString(ce));
+    }
+    return VPP_OK;
+}
+
+size_t vpp_block_attn_workspace_size(const vpp_chunk_attn_args* a, int32_t topk) {
+    g_err[0] = 0;
+    BlockPlan b{};
+    return block_plan(a, topk, &b) == VPP_OK ? b.total : 0;
+}
+
+vpp_status vpp_block_attn_fwd(const vpp_chunk_attn_args* a, const int32_t* block_indices, int32_t topk, vpp_stream_t stream_) {
+    g_err[0] = 0;
+    BlockPlan b{};
+    vpp_status st = block_plan(a, topk, &b);
+    if (st != VPP_OK) return st;
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    g_launches = 0;
+    if (a->total_q == 0 || a->num_reqs == 0) return zero_status(a->status, stream);
+    st = check_paged(a->block_table, a->block_size, a->max_blocks_per_req, a->num_blocks);
+    if (st != VPP_OK) return st;
+    if (!a->q || !a->out || !a->k_cache || !a->v_cache || !block_indices || !a->prefix_len || !a->chunk_len)
+        return fail(VPP_ERR_INVALID_ARG, "q, k_cache, v_cache, out, block_indices, prefix_len and chunk_len must be non-null");
+    if (mis16(a->q) || mis16(a->out) || mis16(a->k_cache) || mis16(a->v_cache))
+        return fail(VPP_ERR_INVALID_ARG, "q, out, k_cache and v_cache must be 16-byte aligned");
+    const int64_t strides[6] = {a->k_block_stride, a->k_token_stride, a->k_head_stride, a->v_block_stride, a->v_token_stride, a->v_head_stride};
+    for (int i = 0; i < 6; ++i)
+        if (strides[i] <= 0 || strides[i] % 8 != 0) return fail(VPP_ERR_INVALID_ARG, "cache strides must be positive multiples of 8 elements");
+    if (!a->workspace || a->workspace_bytes < b.total) return fail(VPP_ERR_WORKSPACE, "workspace: need %zu bytes, got %zu", b.total, a->workspace_bytes);
+    if (reinterpret_cast<uintptr_t>(a->workspace) & 255u) return fail(VPP_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+    uint8_t* ws = static_cast<uint8_t*>(a->workspace);
+
+    CUtensorMap tm_q, tm_q1, tm_k, tm_v, tm_kx, tm_vx;
+    vpp::BlkParams p{};
+    {
+        const uint64_t dq[3] = {128, static_cast<uint64_t>(a->num_q_heads), static_cast<uint64_t>(a->total_q)};
+        const uint64_t sq[2] = {256, 256ull * a->num_q_heads};
+        const uint32_t bq[3] = {64, static_cast<uint32_t>(b.group), static_cast<uint32_t>(b.tile_tokens)}, b1[3] = {64, static_cast<uint32_t>(b.group), 1};
+        if (!make_tmap(&tm_q, a->q, 3, dq, sq, bq) || !make_tmap(&tm_q1, a->q, 3, dq, sq, b1)) return fail(VPP_ERR_CUDA, "cuTensorMapEncodeTiled(q) failed");
+        int32_t k_from = INT32_MAX, v_from = INT32_MAX;        // (0: the other map cannot express the strides)
+        if (!make_kv_maps(a->k_cache, a->k_block_stride, a->k_token_stride, a->k_head_stride, a->block_size, a->num_blocks, a->num_kv_heads, a->block_size,
+                          &tm_k, &tm_kx, &p.k_block_units, &p.k_head_units, &p.k_end, &k_from) ||
+            !make_kv_maps(a->v_cache, a->v_block_stride, a->v_token_stride, a->v_head_stride, a->block_size, a->num_blocks, a->num_kv_heads, a->block_size,
+                          &tm_v, &tm_vx, &p.v_block_units, &p.v_head_units, &p.v_end, &v_from))
+            return fail(VPP_ERR_CUDA, "cuTensorMapEncodeTiled(k/v) failed");
+        p.k_exact = k_from == 0;
+        p.v_exact = v_from == 0;
+    }
+    vpp::BlkListParams lp{};
+    lp.indices = block_indices;
+    lp.block_table = a->block_table;
+    lp.prefix_len = a->prefix_len;
+    lp.chunk_len = a->chunk_len;
+    lp.num_reqs = a->num_reqs;
+    lp.max_blocks_per_req = a->max_blocks_per_req;
+    lp.block_shift = ilog2(a->block_size);
+    lp.num_blocks = a->num_blocks;
+    lp.capacity = paged_capacity(a->max_blocks_per_req, a->block_size);
+    if (lp.capacity > a->max_seq_len) lp.capacity = a->max_seq_len;
+    lp.total_q = a->total_q;
+    lp.num_kv_heads = a->num_kv_heads;
+    lp.topk = topk;
+    lp.tile_tokens = b.tile_tokens;
+    lp.words = b.words;
+    lp.max_tiles = b.max_tiles;
+    lp.max_pages = b.max_pages;
+    lp.header = reinterpret_cast<vpp::WorkHeader*>(ws);
+    lp.items = reinterpret_cast<vpp::BlkItem*>(ws + b.items);
+    lp.pages = reinterpret_cast<int2*>(ws + b.pages);
+    lp.masks = reinterpret_cast<uint32_t*>(ws + b.masks);
+    lp.status = a->status;
+    const size_t lens = 2 * sizeof(int32_t) * (static_cast<size_t>(a->num_reqs) + 1);
+    cudaError_t ce = cudaFuncSetAttribute(vpp::block_lists_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lens));
+    if (ce == cudaSuccess) ce = cudaFuncSetAttribute(vpp::attn_blk_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, vpp::kBlkSmem);
+    if (ce != cudaSuccess) return fail(VPP_ERR_CUDA, "block-sparse attention attributes: %s", cudaGetErrorString(ce));
+    const unsigned tiles = static_cast<unsigned>(b.max_tiles) * a->num_kv_heads;
+    ce = launch(vpp::block_lists_kernel, tiles, vpp::kBlkListThreads, lens, stream, lp);
+    if (ce != cudaSuccess) return fail(VPP_ERR_CUDA, "page lists launch: %s", cudaGetErrorString(ce));
+    ++g_launches;
+
+    p.header_ro = p.header = lp.header;
+    p.items = lp.items;
+    p.pages = lp.pages;
+    p.masks = lp.masks;
+    p.max_tiles = b.max_tiles;
+    p.max_pages = b.max_pages;
+    p.words = b.words;
+    p.block_shift = lp.block_shift;
+    p.num_blocks = a->num_blocks;
+    p.num_q_heads = a->num_q_heads;
+    p.num_kv_heads = a->num_kv_heads;
+    p.group = b.group;
+    p.total_q = a->total_q;
+    p.tile_tokens = b.tile_tokens;
+    p.splits = b.splits;
+    p.box_rows = a->block_size;
+    p.scale_log2e = a->softmax_scale * 1.4426950408889634f;
+    p.out = static_cast<uint8_t*>(a->out);
+    p.lse = a->lse;
+    p.o_parts = reinterpret_cast<float*>(ws + b.o_parts);
+    p.lse_parts = reinterpret_cast<float*>(ws + b.lse_parts);
+    p.status = a->status;
+    const long long work = static_cast<long long>(tiles) * b.splits, sms = sm_count_or_default();
+    ce = launch(vpp::attn_blk_kernel, static_cast<unsigned>(work < sms ? work : sms), vpp::kWsThreads, vpp::kBlkSmem, stream, tm_q, tm_q1,
+                p.k_exact ? tm_kx : tm_k, p.v_exact ? tm_vx : tm_v, p);
+    if (ce != cudaSuccess) return fail(VPP_ERR_CUDA, "block-sparse attention launch: %s", cudaGetErrorString(ce));
+    ++g_launches;
+    if (b.splits > 1) {
+        ce = launch_merge(p.o_parts, p.lse_parts, b.splits, a->total_q, a->num_q_heads, 128, lp.header, a->out, a->lse, stream);
+        if (ce != cudaSuccess) return fail(VPP_ERR_CUDA, "merge launch: %s", cudaGetErrorString(ce));
+        ++g_launches;
     }
     return VPP_OK;
 }

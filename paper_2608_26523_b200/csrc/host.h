@@ -9,6 +9,7 @@
 #include "../../include/vpp.h"
 
 namespace vpp {
+struct WorkHeader;
 namespace host {
 
 extern thread_local char g_err[512];      // vpp_last_error
@@ -30,6 +31,10 @@ inline int ilog2(int x) {
 bool make_tmap(CUtensorMap* m, const void* base, int rank, const uint64_t* dims, const uint64_t* strides_bytes, const uint32_t* box);
 bool make_kv_maps(const void* base, int64_t block_stride, int64_t token_stride, int64_t head_stride, int B, int n_blocks, int heads, int box_rows,
                   CUtensorMap* tm, CUtensorMap* tm_exact, int32_t* block_units, int32_t* head_units, int32_t* end, int32_t* exact_from);
+
+// Every row's `splits` partial results joined (merge.cuh); nothing where the header has an error.
+cudaError_t launch_merge(const float* o_parts, const float* lse_parts, int splits, int total_q, int num_q_heads, int head_dim_v,
+                         const WorkHeader* header, void* out, float* lse, cudaStream_t stream);
 
 // Launch with programmatic stream serialization: the kernel may start (and set itself up) while its predecessor in the
 // stream still runs, and waits for it (griddepcontrol.wait) before it touches memory.
