@@ -738,7 +738,7 @@ attn_blk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                 if (p.splits == 1) {
                     if (p.lse) p.lse[orow] = lse;
                 } else {
-                    p.lse_parts[prow] = lse;
+                    p.lse_parts[prow] = lse == lse ? lse : INFINITY;      // (the merge takes the largest: a NaN would be lost beside parts without keys)
                 }
             }
             tc_fence_before();

@@ -208,7 +208,7 @@ __global__ void __launch_bounds__(kSelectThreads) block_scores_kernel(const Sele
                 const bool fine = e[i] >= 0 && e[i] < p.num_blocks;
                 bad |= !fine;
                 x[i] = make_uint4(0, 0, 0, 0);
-                if (j < page1 && fine) x[i] = ld_once(p.means + (static_cast<long long>(e[i]) * p.num_kv_heads + g) * 256 + v * 16);
+                if (j < page1 && j >= p.num_first && fine) x[i] = ld_once(p.means + (static_cast<long long>(e[i]) * p.num_kv_heads + g) * 256 + v * 16);
             }
 #pragma unroll
             for (int i = 0; i < kDeep; ++i) {
@@ -262,8 +262,8 @@ __global__ void __launch_bounds__(kSelectThreads) block_scores_kernel(const Sele
             const int j = j0 + (tid >> 4) + 16 * i;
             const bool fine = e[i] >= 0 && e[i] < p.num_blocks;
             bad |= !fine;
-            x[i] = make_uint4(0, 0, 0, 0);
-            if (j < page1 && fine) x[i] = ld_once(p.means + (static_cast<long long>(e[i]) * p.num_kv_heads + g) * 256 + v * 16);
+            x[i] = make_uint4(0, 0, 0, 0);        // (pages that are taken anyway count as 0: what theirs hold must not widen the bound)
+            if (j < page1 && j >= p.num_first && fine) x[i] = ld_once(p.means + (static_cast<long long>(e[i]) * p.num_kv_heads + g) * 256 + v * 16);
         }
     };
     for (int t = tid >> 4; t < n; t += kSelectThreads / 16) {
