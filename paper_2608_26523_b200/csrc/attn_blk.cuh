@@ -9,13 +9,18 @@
 //    Neighbours' lists mostly agree, so the union is little longer than a list; one of few tokens stays so where they agree less
 //    (that is why a tile is one accumulator tile, not two as in the dense kernel: 8 tokens of groups of 16, not 16).
 //
-// One Q tile, two softmax groups of four warps that take the KV steps in turn, each an online softmax of its own with its own scores
-// and accumulator in tensor memory (S_0 | S_1 | O_0 | O_1): while one group works on its scores the tensor core runs the other's products.
-// At the end both join the two results, half the features each.  Q has two buffers, so that the next item's first scores are
-// formed under the join.
+// One Q tile, two softmax groups of four warps: of every step's 128 keys group 0 takes the first 64 and group 1 the others, each an online softmax of its
+// own with an accumulator of its own.  Scores have two buffers in tensor memory (S 128 columns | S 128 | O_0 | O_1), so that the groups work on
+// one step's while the tensor core runs P V of the last and forms the next.  The scores of both groups are one MMA chain of 128 keys, and a step has two commits: "scores"
+// (also: the K stage and Q are free) and "P V" (also: the V stage is free, O is quiet).  Tried before, 4096 tokens of 64/4 heads with 34 steps a tile:
+// whole steps in turn, one buffer a group, 690 us (a group waits 1900 clk for its next scores); a chain of 64 keys and commits of its own for each
+// group, 690 us (2500 clk a step, 1800 of them the issue of 24 MMAs and 4 commits).  At the end both join the two results, half the features
+// each.  Q has two buffers, so that the next item's first scores are formed under the join.
+// A page is listed or not by a token as a whole, so the mask of most steps is a bit per row and 16 columns: it is applied to the weights' words, the sums
+// and the maxima of 16 columns, not to every score; the own page, which is seen in part, goes through the scores.
 //   warp 0      scheduler, K producer      warp 1  the thread that issues the MMAs
 //   warp 2      V producer, tensor memory  warps 4-7, 8-11  softmax groups
-// Every wait is bounded, as in attn_ws.cuh, whose hand-overs of P in parts, lazy rescale and packed fma this kernel has too.
+// Every wait is bounded, as in attn_ws.cuh, whose lazy rescale and packed fma this kernel has too.
 #pragma once
 #include <cstdint>
 
@@ -28,8 +33,7 @@ namespace vpp {
 
 constexpr int kBlkListThreads = 128;
 constexpr int kBlkWindow = 8192;              // mask words of a window of pages
-constexpr int kBlkMaxPages = 8;               // pages of a step (128 keys, pages of 16)
-constexpr int kBlkInfo = 8;                   // steps whose masks are in shared memory
+constexpr int kBlkHalfPages = 4;              // pages of a group's 64 keys, at most (pages of 16)
 
 // One query tile and kv-head.
 struct __align__(16) BlkItem {
@@ -54,8 +58,8 @@ struct BlkListParams {
     int max_tiles, max_pages;     // tiles of the launch and pages of a union, at most
     WorkHeader* header;           // num_units: tiles; error; counter
     BlkItem* items;               // [Hkv, max_tiles]
-    int2* pages;                  // [Hkv, max_tiles, max_pages]: physical, logical
-    uint32_t* masks;              // [Hkv, max_tiles, max_pages, words]
+    int32_t* pages;               // [Hkv, max_tiles, max_pages]: physical
+    uint2* masks;                 // [Hkv, max_tiles, max_pages, words]: logical, tokens
     int32_t* status;
 };
 
@@ -109,8 +113,8 @@ __global__ void __launch_bounds__(kBlkListThreads) block_lists_kernel(const BlkL
     const int32_t* const lists = p.indices + (static_cast<long long>(row0) * p.num_kv_heads + g) * p.topk;
     const int32_t* const table = p.block_table + static_cast<long long>(r) * p.max_blocks_per_req;
     const long long item = static_cast<long long>(g) * p.max_tiles + tile;
-    int2* const pages = p.pages + item * p.max_pages;
-    uint32_t* const masks = p.masks + item * p.max_pages * p.words;
+    int32_t* const pages = p.pages + item * p.max_pages;
+    uint2* const masks = p.masks + item * p.max_pages * p.words;
     const int W = p.words, window = kBlkWindow / W, entries = tokens * p.topk;
     int count = 0;            // pages so far
     int last = -1;            // the last of them
@@ -150,8 +154,8 @@ __global__ void __launch_bounds__(kBlkListThreads) block_lists_kernel(const BlkL
                 const int e = __ldg(table + w0 + i);
                 const bool fine = e >= 0 && e < p.num_blocks;
                 if (!fine) s_bad = 1;
-                pages[k] = make_int2(fine ? e : p.num_blocks, w0 + i);       // (num_blocks: reads as zero)
-                for (int w = 0; w < W; ++w) masks[static_cast<long long>(k) * W + w] = fine ? s_mask[i * W + w] : 0;
+                pages[k] = fine ? e : p.num_blocks;       // (num_blocks: reads as zero)
+                for (int w = 0; w < W; ++w) masks[static_cast<long long>(k) * W + w] = make_uint2(w0 + i, fine ? s_mask[i * W + w] : 0);
             }
             at += __popc(m);
             if (m) last = w0 + i0 + 31 - __clz(m);
@@ -168,8 +172,8 @@ struct BlkParams {
     const WorkHeader* header_ro;
     WorkHeader* header;
     const BlkItem* items;
-    const int2* pages;
-    const uint32_t* masks;
+    const int32_t* pages;
+    const uint2* masks;
     int max_tiles, max_pages, words;
     int block_shift, num_blocks;
     int num_q_heads, num_kv_heads, group;
@@ -197,36 +201,44 @@ struct BlkWork {
     long long list;               // first page of the union
 };
 
-// masks of a step: pages' logical numbers and tokens
-struct BlkInfo {
-    int32_t page[kBlkMaxPages];
-    uint32_t mask[kBlkMaxPages][4];
-};
-
-constexpr int kBlkStages = 4;
-constexpr int kBlkBars = (2 + kBlkStages) * kTileBytes;        // offset of what follows the tiles
-constexpr int kBlkOffInfo = 512, kBlkOffStat = kBlkOffInfo + kBlkInfo * static_cast<int>(sizeof(BlkInfo));
-constexpr int kBlkSmem = kBlkBars + kBlkOffStat + 2 * 2 * 128 * 4 + 1024 /* alignment */;
+constexpr int kBlkBars = 6 * kTileBytes;      // offset of what follows the tiles: two of Q, two stages of K and V each
+constexpr int kBlkOffStat = 512, kBlkOffStage = kBlkOffStat + 2 * 2 * 128 * 4, kBlkStageBytes = 2048;
+constexpr int kBlkSmem = kBlkBars + kBlkOffStage + 8 * kBlkStageBytes + 1024 /* alignment */;
 static_assert(kBlkSmem <= 232448, "shared memory of one CTA");
 
-// The keys of columns 32 w .. 32 w + 31 of a step that a token sees.
-__device__ __forceinline__ uint32_t blk_visible(const BlkInfo& f, int w, int shift, int tok, int own, int own_off) {
-    const int word = tok >> 5, bit = tok & 31;
-    if (shift >= 5) {
-        const int s = (w * 32) >> shift, first = (w * 32) & ((1 << shift) - 1);
-        if (!((f.mask[s][word] >> bit) & 1)) return 0;
-        const int lim = f.page[s] == own ? own_off - first : 31;
-        return lim >= 31 ? 0xffffffffu : lim < 0 ? 0u : (2u << lim) - 1;
+// What a token sees of a group's 64 keys: a bit for each 16 of them (bits 0 .. 3), and `lim`, the last key seen where the own page is among them (else >= 63).
+// f: the group's pages of the step, logical number and the word of the mask that has the token.
+__device__ __forceinline__ uint32_t blk_visible(const uint2 (&f)[kBlkHalfPages], int t, int shift, int bit, int own, int own_off, int& lim) {
+    lim = 64;
+    if (shift >= 6) {                        // one page
+        if (static_cast<int>(f[0].x) == own) lim = own_off - ((t * 64) & ((1 << shift) - 1));
+        return (f[0].y >> bit) & 1 && lim >= 0 ? 15u : 0u;
     }
     uint32_t v = 0;
+    const int n = 64 >> shift;               // two or four pages
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int s = 2 * w + h;
-        if (!((f.mask[s][word] >> bit) & 1)) continue;
-        const int lim = f.page[s] == own ? own_off : 15;
-        v |= ((2u << lim) - 1) << (16 * h);
+    for (int i = 0; i < kBlkHalfPages; ++i) {
+        if (i >= n || !((f[i].y >> bit) & 1)) continue;
+        v |= (shift == 5 ? 3u : 1u) << (shift == 5 ? 2 * i : i);
+        if (static_cast<int>(f[i].x) == own) lim = (i << shift) + own_off;      // (the last page that the token lists: none behind it)
     }
     return v;
+}
+// A warp's 32 rows x 64 bytes (lane l holds row l) to global memory, whole runs of 64 bytes, through 2 KB of the warp's own.  (Straight from the registers a
+// store of 16 bytes a lane touches 32 lines: 4000 clk for the join of an item.)
+template <typename RowOf>
+__device__ __forceinline__ void blk_flush(uint8_t* stage, const uint4 (&v)[4], RowOf row_of) {
+    const int lane = threadIdx.x & 31;
+    __syncwarp();
+#pragma unroll
+    for (int q = 0; q < 4; ++q) *reinterpret_cast<uint4*>(stage + lane * 64 + ((q ^ ((lane >> 1) & 3)) << 4)) = v[q];
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = 8 * i + (lane >> 2), q = lane & 3;
+        uint8_t* const dst = row_of(r);
+        if (dst) *reinterpret_cast<uint4*>(dst + q * 16) = *reinterpret_cast<const uint4*>(stage + r * 64 + ((q ^ ((r >> 1) & 3)) << 4));
+    }
 }
 
 __global__ void __launch_bounds__(kWsThreads, 1)
@@ -240,19 +252,17 @@ attn_blk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
     const uint32_t sQ = base, sKV = base + 2 * kTileBytes, sBar = base + kBlkBars;
     const uint32_t bar_item_full = sBar, bar_item_empty = sBar + 16;       // [2]
     const uint32_t bar_q_full = sBar + 32, bar_q_empty = sBar + 48;        // [2]
-    const uint32_t bar_s_full = sBar + 64, bar_p_full = sBar + 80;         // [2]
-    const uint32_t bar_o_full = sBar + 96;                                 // [2]
-    const uint32_t bar_p_part = sBar + 112;                                // [2][2]: after 32 and after 64 columns
-    const uint32_t bar_kv_full = sBar + 144, bar_kv_empty = sBar + 176;    // [kBlkStages]
+    const uint32_t bar_s = sBar + 64;                                      // [2] scores of a buffer
+    const uint32_t bar_p = sBar + 80;                                      // [2] weights of a buffer, of both groups
+    const uint32_t bar_pv = sBar + 112;                                    // [2] both groups' products of a step, by its buffer
+    const uint32_t bar_kv_full = sBar + 144;                               // [2][K, V]
     const uint32_t bar_vfix = sBar + 208;                                  // [2]
-    const uint32_t bar_info = sBar + 224;                                  // [kBlkInfo]
     const uint32_t bar_stat = sBar + 288, bar_done = sBar + 296;
     uint8_t* const gen_bar = gen + kBlkBars;
     volatile int* const s_abort = reinterpret_cast<volatile int*>(gen_bar + 304);
     volatile uint32_t* const s_tmem = reinterpret_cast<volatile uint32_t*>(gen_bar + 308);
     BlkWork* const ring = reinterpret_cast<BlkWork*>(gen_bar + 320);       // [2]
-    static_assert(320 + 2 * sizeof(BlkWork) <= kBlkOffInfo, "item ring");
-    BlkInfo* const info = reinterpret_cast<BlkInfo*>(gen_bar + kBlkOffInfo);
+    static_assert(320 + 2 * sizeof(BlkWork) <= kBlkOffStat, "item ring");
     float* const stat = reinterpret_cast<float*>(gen_bar + kBlkOffStat);   // [group][m, l][128]
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -262,18 +272,13 @@ attn_blk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             mbar_init(bar_item_empty + 8 * i, 10);      // 8 softmax warps, the MMA thread, the V producer
             mbar_init(bar_q_full + 8 * i, 1);
             mbar_init(bar_q_empty + 8 * i, 1);
-            mbar_init(bar_s_full + 8 * i, 1);
-            mbar_init(bar_p_full + 8 * i, 4);
-            mbar_init(bar_o_full + 8 * i, 1);
-            mbar_init(bar_p_part + 8 * i, 4);
-            mbar_init(bar_p_part + 16 + 8 * i, 4);
+            mbar_init(bar_s + 8 * i, 1);
+            mbar_init(bar_pv + 8 * i, 1);
+            mbar_init(bar_p + 8 * i, 8);
+            mbar_init(bar_kv_full + 8 * i, 1);
+            mbar_init(bar_kv_full + 16 + 8 * i, 1);
             mbar_init(bar_vfix + 8 * i, 1);
         }
-        for (int i = 0; i < kBlkStages; ++i) {
-            mbar_init(bar_kv_full + 8 * i, 1);
-            mbar_init(bar_kv_empty + 8 * i, 1);
-        }
-        for (int i = 0; i < kBlkInfo; ++i) mbar_init(bar_info + 8 * i, 1);
         mbar_init(bar_stat, 8);
         mbar_init(bar_done, 8);
         fence_mbar_init();
@@ -301,14 +306,16 @@ attn_blk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
 
     if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kWsRegsLow));
-        // One K (which = 0) or V tile into ring stage it % kBlkStages: `phys` is the page of the lane's copy.
-        auto load_tile = [&](int which, uint32_t it, int g, int phys) -> bool {
-            const uint32_t st = it % kBlkStages, full = bar_kv_full + 8 * st;
+        // The K (which = 0) or V tile of step `step` (counted over all items): `phys` is the page of the lane's copy.
+        auto load_tile = [&](int which, uint32_t step, int g, int phys) -> bool {
+            const uint32_t st = 2 * (step & 1) + which, full = bar_kv_full + 8 * st;
             const bool exact = which == 0 ? p.k_exact : p.v_exact;
             const int rows = exact ? kExactRows : p.box_rows, off = lane * rows;
             bool ok = true;
             if (lane == 0) {
-                ok = mbar_wait(bar_kv_empty + 8 * st, ((it / kBlkStages) & 1) ^ 1, s_abort, 603 + which);
+                // the stage's last user: the scores, or the products, of two steps ago
+                // (neither barrier can be a phase further: that takes this very tile)
+                if (step >= 2) ok = mbar_wait((which == 0 ? bar_s : bar_pv) + 8 * (step & 1), ((step - 2) >> 1) & 1, s_abort, 603 + which);
                 if (ok) mbar_arrive_expect_tx(full, kTileBytes);
             }
             ok = __shfl_sync(0xffffffffu, ok, 0);
@@ -329,7 +336,7 @@ attn_blk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
         };
         if (warp == 0) {
             // ============================ scheduler, K producer ============================
-            uint32_t n_item = 0, it = 0, n_q = 0;
+            uint32_t n_item = 0, step = 0, n_q = 0;
             const int copy_rows = p.k_exact ? kExactRows : p.box_rows;
             while (true) {
                 int k = blockIdx.x;
@@ -386,44 +393,19 @@ attn_blk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                 ok = __shfl_sync(0xffffffffu, ok, 0);
                 if (!ok) break;
                 ++n_q;
-                // entries 32 at a time, a lane each
-                int2 e = make_int2(0, 0);
-                uint32_t m[4] = {};
+                // pages 32 at a time, a lane each
+                int phys_mine = 0;
                 const int e0 = w.begin * per_step;
-                for (int j = w.begin; j < w.end && ok; ++j) {
+                for (int j = w.begin; j < w.end && ok; ++j, ++step) {
                     const int k0 = j * per_step, in = (k0 - e0) & 31;
-                    if (in == 0) {
-                        const int i = k0 + lane;
-                        e = make_int2(p.num_blocks, -1);
-#pragma unroll
-                        for (int x = 0; x < 4; ++x) m[x] = 0;
-                        if (i < w.pages) {
-                            e = p.pages[w.list + i];
-#pragma unroll
-                            for (int x = 0; x < 4; ++x)
-                                if (x < p.words) m[x] = p.masks[(w.list + i) * p.words + x];
-                        }
-                    }
-                    const int phys = __shfl_sync(0xffffffffu, e.x, in + ((lane * copy_rows) >> shift));
-                    ok = load_tile(0, it, w.g, phys);
-                    if (!ok) break;
-                    // (the stage is free, so the softmax has read the masks of four steps ago)
-                    const uint32_t s = (it >> 1) % kBlkInfo;
-                    if (lane >= in && lane < in + per_step) {
-                        info[s].page[lane - in] = e.y;
-#pragma unroll
-                        for (int x = 0; x < 4; ++x)
-                            if (x < p.words) info[s].mask[lane - in][x] = m[x];
-                    }
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(bar_info + 8 * s);
-                    it += 2;
+                    if (in == 0) phys_mine = k0 + lane < w.pages ? p.pages[w.list + k0 + lane] : p.num_blocks;
+                    ok = load_tile(0, step, w.g, __shfl_sync(0xffffffffu, phys_mine, in + ((lane * copy_rows) >> shift)));
                 }
                 if (!ok) break;
             }
         } else if (warp == 2) {
             // ============================ V producer ============================
-            uint32_t n_item = 0, it = 0, fixes = 0;
+            uint32_t n_item = 0, step = 0, fixes = 0;
             const int copy_rows = p.v_exact ? kExactRows : p.box_rows;
             while (true) {
                 const uint32_t slot = n_item & 1;
@@ -440,14 +422,13 @@ attn_blk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                 const int e0 = w.begin * per_step, steps = (w.pages + per_step - 1) / per_step;
                 for (int j = w.begin; j < w.end && ok; ++j) {
                     const int k0 = j * per_step, in = (k0 - e0) & 31;
-                    if (in == 0) phys_mine = k0 + lane < w.pages ? p.pages[w.list + k0 + lane].x : p.num_blocks;
-                    const int phys = __shfl_sync(0xffffffffu, phys_mine, in + ((lane * copy_rows) >> shift));
-                    ok = load_tile(1, it + 1, w.g, phys);
+                    if (in == 0) phys_mine = k0 + lane < w.pages ? p.pages[w.list + k0 + lane] : p.num_blocks;
+                    ok = load_tile(1, step, w.g, __shfl_sync(0xffffffffu, phys_mine, in + ((lane * copy_rows) >> shift)));
                     if (!ok) break;
                     if (w.last_keys != 0 && j == steps - 1) {
                         // slots past the end hold anything: their values become 0, so that 0 * garbage cannot reach O.  The MMA thread waits for it.
-                        const uint32_t st = (it + 1) % kBlkStages;
-                        if (lane == 0) ok = mbar_wait(bar_kv_full + 8 * st, ((it + 1) / kBlkStages) & 1, s_abort, 612);
+                        const uint32_t st = 2 * (step & 1) + 1;
+                        if (lane == 0) ok = mbar_wait(bar_kv_full + 8 * st, (step >> 1) & 1, s_abort, 612);
                         ok = __shfl_sync(0xffffffffu, ok, 0);
                         if (!ok) break;
                         uint8_t* const vb = gen + 2 * kTileBytes + st * kTileBytes;
@@ -467,7 +448,7 @@ attn_blk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                         if (lane == 0) mbar_arrive(bar_vfix + 8 * (fixes & 1));
                         ++fixes;
                     }
-                    it += 2;
+                    ++step;
                 }
                 if (!ok) break;
             }
@@ -475,7 +456,7 @@ attn_blk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             // ============================ MMA issuer (a single thread) ============================
             constexpr uint32_t kIdescQK = idesc_bf16(128, 128, false, false), kIdescPV = idesc_bf16(128, 128, false, true);
             constexpr uint32_t kHiQ = desc_hi_sw128(1024), kHiKV = desc_hi_sw128(kGroupBytes);
-            uint32_t n_item = 0, n_q = 0, it = 0, fixes = 0, p_it0 = 0, p_it1 = 0;
+            uint32_t n_item = 0, n_q = 0, step = 0, fixes = 0;
             auto wait = [&](uint32_t bar, uint32_t parity, int where) { return mbar_wait(bar, parity, s_abort, where); };
             while (true) {
                 const uint32_t slot = n_item & 1;
@@ -489,56 +470,52 @@ attn_blk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                 const uint32_t qb = n_q & 1;
                 if (!wait(bar_q_full + 8 * qb, (n_q >> 1) & 1, 622)) break;
                 ++n_q;
-                const uint32_t q_lo = desc_lo_sw128(sQ + qb * kTileBytes, 16), first = it;
-                // step j takes ring entries first + 2 j (K) and first + 2 j + 1 (V), and group j & 1
-                auto scores = [&](int j) -> bool {
-                    const uint32_t idx = first + 2 * j, st = idx % kBlkStages;
-                    if (!wait(bar_kv_full + 8 * st, (idx / kBlkStages) & 1, 623)) return false;
-                    tc_fence_after();
-                    const uint32_t k_lo = desc_lo_sw128(sKV + st * kTileBytes, 16), tS = tmem + (j & 1) * 128;
+                const uint32_t q_lo = desc_lo_sw128(sQ + qb * kTileBytes, 16), first = step;
+                auto have_k = [&](int j) { return wait(bar_kv_full + 16 * ((first + j) & 1), ((first + j) >> 1) & 1, 623); };
+                auto scores = [&](int j) {
+                    const uint32_t buf = (first + j) & 1, st = 2 * buf;
+                    const uint32_t k_lo = desc_lo_sw128(sKV + st * kTileBytes, 16), tS = tmem + buf * 128;
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
                         const uint32_t qoff = ((k >> 2) * kSlabBytes + (k & 3) * 32) >> 4, koff = ((k >> 2) * kHalfBytes + (k & 3) * 32) >> 4;
                         mma_ss_lhh(tS, q_lo + qoff, kHiQ, k_lo + koff, kHiKV, kIdescQK, k > 0);
                     }
-                    tc_commit(bar_s_full + 8 * (j & 1));
-                    tc_commit(bar_kv_empty + 8 * st);
+                    tc_commit(bar_s + 8 * buf);
                     if (j + 1 == n) tc_commit(bar_q_empty + 8 * qb);
-                    return true;
                 };
-                bool ok = scores(0);
-                if (ok && n > 1) ok = scores(1);
+                bool ok = have_k(0);
+                if (!ok) break;
+                tc_fence_after();
+                scores(0);
+                if (n > 1) {
+                    ok = have_k(1);
+                    if (!ok) break;
+                    scores(1);
+                }
                 for (int j = 0; j < n && ok; ++j) {
-                    const int t = j & 1;
-                    const uint32_t idx = first + 2 * j + 1, st = idx % kBlkStages, pit = t ? p_it1 : p_it0;
-                    ok = wait(bar_kv_full + 8 * st, (idx / kBlkStages) & 1, 624);
+                    const uint32_t buf = (first + j) & 1, parity = ((first + j) >> 1) & 1, st = 2 * buf + 1;
+                    ok = wait(bar_kv_full + 8 * st, parity, 624);
                     if (!ok) break;
                     if (mend && j == n - 1) {
                         ok = wait(bar_vfix + 8 * (fixes & 1), (fixes >> 1) & 1, 625);
                         if (!ok) break;
                         ++fixes;
                     }
-                    const uint32_t tP = tmem + t * 128, tO = tmem + 256 + t * 128, v_lo = desc_lo_sw128(sKV + st * kTileBytes, kHalfBytes);
-                    int k0 = 0;
-#pragma unroll
-                    for (int c = 0; c < 3; ++c) {
-                        ok = wait(c < 2 ? bar_p_part + 16 * c + 8 * t : bar_p_full + 8 * t, pit & 1, 626 + c);
-                        if (!ok) break;
-                        tc_fence_after();
-                        const int k1 = c < 2 ? 2 * (c + 1) : 8;
-#pragma unroll
-                        for (int k = 0; k < 8; ++k)
-                            if (k >= k0 && k < k1) mma_ts_lh(tO, tP + k * 8, v_lo + k * (2 * kGroupBytes >> 4), kHiKV, kIdescPV, (j >= 2 || k > 0) ? 1u : 0u);
-                        k0 = k1;
-                    }
+                    if (j + 2 < n) ok = have_k(j + 2);      // (before the waits for P: a wait that is over takes 90 clk too)
                     if (!ok) break;
-                    tc_commit(bar_kv_empty + 8 * st);
-                    if (t) ++p_it1; else ++p_it0;
-                    if (j + 2 < n) ok = scores(j + 2);
-                    else tc_commit(bar_o_full + 8 * t);
+                    ok = wait(bar_p + 8 * buf, parity, 626);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t tP = tmem + buf * 128, v_lo = desc_lo_sw128(sKV + st * kTileBytes, kHalfBytes);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        mma_ts_lh(tmem + 256 + (k >> 2) * 128, tP + (k >> 2) * 64 + (k & 3) * 8, v_lo + k * (2 * kGroupBytes >> 4), kHiKV, kIdescPV,
+                                  (j > 0 || (k & 3) > 0) ? 1u : 0u);
+                    tc_commit(bar_pv + 8 * buf);
+                    if (j + 2 < n) scores(j + 2);
                 }
                 if (!ok) break;
-                it = first + 2 * n;
+                step = first + n;
             }
         }
         // warp 3 has nothing to do until teardown
@@ -547,10 +524,10 @@ attn_blk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kWsRegsHigh));
         const int t = (warp - 4) >> 2, row = ((warp & 3) << 5) | lane;
         const uint32_t lane_off = static_cast<uint32_t>((warp & 3) * 32) << 16;
-        const uint32_t tS = tmem + t * 128 + lane_off, tO = tmem + 256 + t * 128 + lane_off;
+        const uint32_t tS0 = tmem + t * 64 + lane_off, tO = tmem + 256 + t * 128 + lane_off;
         const float sc = p.scale_log2e;
         const int my_tok = row / p.group, my_head = row - my_tok * p.group;
-        uint32_t n_item = 0, s_it = 0, o_it = 0, x_it = 0, step0 = 0;      // step0: steps of the items before
+        uint32_t n_item = 0, x_it = 0, step = 0;      // step: those of all items
         while (true) {
             const uint32_t slot = n_item & 1;
             if (!mbar_wait(bar_item_full + 8 * slot, (n_item >> 1) & 1, s_abort, 631)) break;
@@ -565,19 +542,39 @@ attn_blk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             const int tok = live ? my_tok : 0;
             float m_ref = -INFINITY, l_run = 0.f;
             bool ok = true, seen = false;
-            for (int j = t; j < n; j += 2) {
-                const uint32_t step = step0 + j, slot_i = step % kBlkInfo;
-                ok = mbar_wait(bar_info + 8 * slot_i, (step / kBlkInfo) & 1, s_abort, 632);
-                if (!ok) break;
-                uint32_t vis[4];
+            // the pages and masks of a step are requested a step ahead
+            uint2 next[kBlkHalfPages];
+            const uint2* at = p.masks + (w.list + static_cast<long long>(w.begin) * per_step + ((t * 64) >> shift)) * p.words + (tok >> 5);
+            int left = w.pages - w.begin * per_step - ((t * 64) >> shift);      // pages of the union from `at` on
+            const int stride = per_step * p.words;
+            auto request = [&]() {
+                next[0] = make_uint2(0, 0);
+                if (left > 0) next[0] = __ldg(at);
+                if (shift < 6) {
 #pragma unroll
-                for (int c = 0; c < 4; ++c) vis[c] = live ? blk_visible(info[slot_i], c, shift, tok, own, own_off) : 0u;
-                const bool mine = (vis[0] | vis[1] | vis[2] | vis[3]) != 0;
+                    for (int i = 1; i < kBlkHalfPages; ++i) {
+                        next[i] = make_uint2(0, 0);
+                        if (i < (64 >> shift) && left > i) next[i] = __ldg(at + i * p.words);
+                    }
+                }
+                at += stride;
+                left -= per_step;
+            };
+            request();
+            for (int j = 0; j < n && ok; ++j, ++step) {
+                const uint32_t buf = step & 1, parity = (step >> 1) & 1, tS = tS0 + buf * 128;
+                int now_lim = 64;
+                const uint32_t now = live ? blk_visible(next, t, shift, tok & 31, own, own_off, now_lim) : 0u;
+                request();
+                const bool mine = now != 0;
                 seen |= mine;
                 const bool none = !__any_sync(0xffffffffu, mine);
-                ok = mbar_wait(bar_s_full + 8 * t, s_it & 1, s_abort, 633);
+                ok = mbar_wait(bar_s + 8 * buf, parity, s_abort, 633);
                 if (!ok) break;
-                ++s_it;
+                if (j == 0 && x_it > 0) {      // the last item's accumulators are read by both groups before P V overwrites them
+                    ok = mbar_wait(bar_done, (x_it - 1) & 1, s_abort, 638);
+                    if (!ok) break;
+                }
                 tc_fence_after();
                 if (none) {
                     // no row of this warp sees a key of this step
@@ -585,110 +582,97 @@ attn_blk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
 #pragma unroll
                     for (int i = 0; i < 32; ++i) z[i] = 0;
                     tmem_st32(tS, z);
-                    tmem_st32(tS + 32, z);
-                    tc_wait_st();
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) {
-                        mbar_arrive(bar_p_part + 8 * t);
-                        mbar_arrive(bar_p_part + 16 + 8 * t);
-                        mbar_arrive(bar_p_full + 8 * t);
+                } else {
+                    uint32_t s[64];
+                    tmem_ld32(tS, reinterpret_cast<uint32_t(&)[32]>(s[0]));
+                    tmem_ld32(tS + 32, reinterpret_cast<uint32_t(&)[32]>(s[32]));
+                    tc_wait_ld(reinterpret_cast<uint32_t(&)[32]>(s[0]));
+                    tc_wait_ld(reinterpret_cast<uint32_t(&)[32]>(s[32]));
+                    if (__any_sync(0xffffffffu, mine && now_lim < 63)) {
+#pragma unroll
+                        for (int i = 0; i < 64; ++i)
+                            if (mine && i > now_lim) s[i] = 0xff800000u;  // -inf
                     }
-                    continue;
-                }
-                uint32_t s[128];
-                float mx[8];
-                tmem_ld32(tS, reinterpret_cast<uint32_t(&)[32]>(s[0]));
-                tmem_ld32(tS + 32, reinterpret_cast<uint32_t(&)[32]>(s[32]));
-                tc_wait_ld(reinterpret_cast<uint32_t(&)[32]>(s[0]));
-                tc_wait_ld(reinterpret_cast<uint32_t(&)[32]>(s[32]));
-                tmem_ld32(tS + 64, reinterpret_cast<uint32_t(&)[32]>(s[64]));
-                tmem_ld32(tS + 96, reinterpret_cast<uint32_t(&)[32]>(s[96]));
+                    // the largest of the 16-column pieces that are seen
+                    float mxa = -INFINITY;
 #pragma unroll
-                for (int hh = 0; hh < 2; ++hh) {
-                    if (hh == 1) {
-                        tc_wait_ld(reinterpret_cast<uint32_t(&)[32]>(s[64]));
-                        tc_wait_ld(reinterpret_cast<uint32_t(&)[32]>(s[96]));
+                    for (int u = 0; u < 4; ++u) {
+                        float mx[4];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) mx[k] = fmax3(__uint_as_float(s[u * 16 + k]), __uint_as_float(s[u * 16 + 4 + k]), __uint_as_float(s[u * 16 + 8 + k]));
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) mx[k] = fmax3(mx[k], mx[k + 2], __uint_as_float(s[u * 16 + 12 + k]));
+                        const float x = fmax3(fmaxf(mx[0], mx[1]), __uint_as_float(s[u * 16 + 14]), __uint_as_float(s[u * 16 + 15]));
+                        mxa = (now >> u) & 1 ? fmaxf(mxa, x) : mxa;
                     }
-#pragma unroll
-                    for (int c = 2 * hh; c < 2 * hh + 2; ++c)
-                        if (__any_sync(0xffffffffu, vis[c] != 0xffffffffu)) {
-#pragma unroll
-                            for (int i = 0; i < 32; ++i)
-                                if (!((vis[c] >> i) & 1)) s[c * 32 + i] = 0xff800000u;  // -inf
-                        }
-#pragma unroll
-                    for (int i = 0; i < 64; i += 16)
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) {
-                            const float v0 = __uint_as_float(s[hh * 64 + i + k]), v1 = __uint_as_float(s[hh * 64 + i + 8 + k]);
-                            mx[k] = (hh == 0 && i == 0) ? fmaxf(v0, v1) : fmax3(mx[k], v0, v1);
-                        }
-                }
-                const float mxa = fmaxf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), fmaxf(fmaxf(mx[4], mx[5]), fmaxf(mx[6], mx[7])));
-                const float m_new = fmaxf(mxa * sc, m_ref);
-                const bool grow = (m_new - m_ref > kRescaleThreshold) || (m_ref == -INFINITY && m_new != -INFINITY);
-                if (__any_sync(0xffffffffu, grow)) {
-                    const float alpha = grow ? ex2(m_ref - m_new) : 1.f;  // m_ref = -inf gives 0
-                    if (grow) m_ref = m_new;
-                    l_run *= alpha;
-                    if (j >= 2) {   // O of this group already holds something
-                        uint32_t o[32];
+                    const float m_new = fmaxf(mxa * sc, m_ref);
+                    const bool grow = (m_new - m_ref > kRescaleThreshold) || (m_ref == -INFINITY && m_new != -INFINITY);
+                    if (__any_sync(0xffffffffu, grow)) {
+                        const float alpha = grow ? ex2(m_ref - m_new) : 1.f;  // m_ref = -inf gives 0
+                        if (grow) m_ref = m_new;
+                        l_run *= alpha;
+                        if (j > 0) {   // O of this group already holds something
+                            ok = mbar_wait(bar_pv + 8 * (buf ^ 1), ((step - 1) >> 1) & 1, s_abort, 635);      // (the last step's products are still under way)
+                            if (!ok) break;
+                            tc_fence_after();
+                            uint32_t o[32];
 #pragma unroll 1
-                        for (int c = 0; c < 4; ++c) {
-                            tmem_ld32(tO + c * 32, o);
-                            tc_wait_ld(o);
+                            for (int c = 0; c < 4; ++c) {
+                                tmem_ld32(tO + c * 32, o);
+                                tc_wait_ld(o);
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
-                            tmem_st32(tO + c * 32, o);
+                                for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
+                                tmem_st32(tO + c * 32, o);
+                            }
                         }
                     }
-                }
-                const float m_use = (m_ref == -INFINITY) ? 0.f : m_ref;
-                const uint64_t sc2 = pack_f32x2(sc, sc), neg_m2 = pack_f32x2(-m_use, -m_use);
-                float sum0 = 0.f, sum1 = 0.f;
+                    const float m_use = (m_ref == -INFINITY) ? 0.f : m_ref;
+                    const uint64_t sc2 = pack_f32x2(sc, sc), neg_m2 = pack_f32x2(-m_use, -m_use);
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    uint32_t pk[16];
+                    for (int c = 0; c < 2; ++c) {
+                        uint32_t pk[16];
 #pragma unroll
-                    for (int i = 0; i < 32; i += 2) {
-                        float x0, x1;
-                        unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(s[c * 32 + i]), __uint_as_float(s[c * 32 + i + 1])), sc2, neg_m2), x0, x1);
-                        const float p0 = ex2(x0), p1 = ex2(x1);
-                        sum0 += p0;
-                        sum1 += p1;
-                        pk[i >> 1] = pack_bf16x2(p0, p1);
-                        if ((c == 1 || c == 2) && (i >> 1) == kPartWaitDefer - 1) {
-                            tc_wait_st();
-                            tc_fence_before();
-                            __syncwarp();
-                            if (lane == 0) mbar_arrive(bar_p_part + 16 * (c - 1) + 8 * t);
+                        for (int h = 0; h < 2; ++h) {
+                            const uint32_t keep = (now >> (2 * c + h)) & 1 ? 0xffffffffu : 0u;
+                            float sum0 = 0.f, sum1 = 0.f;
+#pragma unroll
+                            for (int i = 0; i < 16; i += 2) {
+                                const int a = c * 32 + h * 16 + i;
+                                float x0, x1;
+                                unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(s[a]), __uint_as_float(s[a + 1])), sc2, neg_m2), x0, x1);
+                                const float p0 = ex2(x0), p1 = ex2(x1);
+                                sum0 += p0;
+                                sum1 += p1;
+                                pk[h * 8 + (i >> 1)] = pack_bf16x2(p0, p1) & keep;
+                            }
+                            l_run += keep ? sum0 + sum1 : 0.f;
                         }
+                        tmem_st16(tS + c * 16, pk);
                     }
-                    tmem_st16(tS + c * 16, pk);
                 }
-                l_run += sum0 + sum1;
                 tc_wait_st();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(bar_p_full + 8 * t);
+                if (lane == 0) mbar_arrive(bar_p + 8 * buf);
             }
             if (!ok) break;
-            step0 += n;
             // ---- the two groups' results joined, half the features each ----
-            if (t < n) {
-                ok = mbar_wait(bar_o_full + 8 * t, o_it & 1, s_abort, 634);
+            if (n > 0) {
+                ok = mbar_wait(bar_pv + 8 * ((step - 1) & 1), ((step - 1) >> 1) & 1, s_abort, 636);
                 if (!ok) break;
-                ++o_it;
             }
             tc_fence_after();
             if (seen && m_ref == -INFINITY && l_run == 0.f) l_run = NAN;        // keys, but all scores -inf: 0 / 0, as the definition has it
+            if (n == 0 && x_it > 0) {          // (an item without steps: as above, before the statistics are overwritten)
+                ok = mbar_wait(bar_done, (x_it - 1) & 1, s_abort, 639);
+                if (!ok) break;
+            }
             stat[t * 256 + row] = m_ref;
             stat[t * 256 + 128 + row] = l_run;
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar_stat);
-            ok = mbar_wait(bar_stat, x_it & 1, s_abort, 635);
+            ok = mbar_wait(bar_stat, x_it & 1, s_abort, 637);
             if (!ok) break;
             tc_fence_after();
             const float m0 = stat[row], l0 = stat[128 + row], m1 = stat[256 + row], l1 = stat[256 + 128 + row];
@@ -706,31 +690,46 @@ attn_blk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             }
             const uint32_t tH = tmem + 256 + lane_off + t * 64;      // this group's features of O_0; O_1's are 128 columns further
             const long long orow = (static_cast<long long>(w.row0) + my_tok) * p.num_q_heads + w.g * p.group + my_head;
+            uint8_t* const stage = gen_bar + kBlkOffStage + (warp - 4) * kBlkStageBytes;
             const long long prow = static_cast<long long>(w.split) * p.total_q * p.num_q_heads + orow;
-#pragma unroll 1
-            for (int c = 0; c < 4; ++c) {        // 16 features at a time
-                uint32_t r[32];                  // (O_0's, O_1's)
-                float v[16];
-                if (n > 0) tmem_ld16(tH + c * 16, reinterpret_cast<uint32_t(&)[16]>(r[0]));
-                if (n > 1) tmem_ld16(tH + 128 + c * 16, reinterpret_cast<uint32_t(&)[16]>(r[16]));
-                tc_wait_ld(r);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {   // (an accumulator without weight is not looked at: 0 * inf)
-                    v[i] = s0 != 0.f && n > 0 ? __uint_as_float(r[i]) * s0 : s0;
-                    if (s1 != 0.f && n > 1) v[i] = fmaf(__uint_as_float(r[16 + i]), s1, v[i]);
+            for (int c = 0; c < 2; ++c) {        // 32 features at a time
+                uint32_t r0[32], r1[32];
+                if (n > 0) {
+                    tmem_ld32(tH + c * 32, r0);
+                    tmem_ld32(tH + 128 + c * 32, r1);
+                    tc_wait_ld(r0);
+                    tc_wait_ld(r1);
                 }
-                if (!live) continue;
+                float v[32];
+#pragma unroll
+                for (int i = 0; i < 32; ++i) {   // (an accumulator without weight is not looked at: 0 * inf)
+                    v[i] = s0 != 0.f && n > 0 ? __uint_as_float(r0[i]) * s0 : s0;
+                    if (s1 != 0.f && n > 0) v[i] = fmaf(__uint_as_float(r1[i]), s1, v[i]);
+                }
                 if (p.splits == 1) {
-                    uint32_t pk[8];
+                    uint4 pk[4];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) pk[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
-                    uint4* const dst = reinterpret_cast<uint4*>(p.out + (orow * 128 + t * 64 + c * 16) * 2);
-                    dst[0] = make_uint4(pk[0], pk[1], pk[2], pk[3]);
-                    dst[1] = make_uint4(pk[4], pk[5], pk[6], pk[7]);
+                    for (int i = 0; i < 4; ++i)
+                        pk[i] = make_uint4(pack_bf16x2(v[8 * i], v[8 * i + 1]), pack_bf16x2(v[8 * i + 2], v[8 * i + 3]), pack_bf16x2(v[8 * i + 4], v[8 * i + 5]),
+                                           pack_bf16x2(v[8 * i + 6], v[8 * i + 7]));
+                    blk_flush(stage, pk, [&](int r) -> uint8_t* {
+                        const long long to = __shfl_sync(0xffffffffu, live ? orow : -1ll, r);
+                        return to < 0 ? nullptr : p.out + (to * 128 + t * 64 + c * 32) * 2;
+                    });
                 } else {
-                    float4* const dst = reinterpret_cast<float4*>(p.o_parts + prow * 128 + t * 64 + c * 16);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) dst[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+                    for (int h = 0; h < 2; ++h) {
+                        uint4 f[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            f[i] = make_uint4(__float_as_uint(v[h * 16 + 4 * i]), __float_as_uint(v[h * 16 + 4 * i + 1]), __float_as_uint(v[h * 16 + 4 * i + 2]),
+                                              __float_as_uint(v[h * 16 + 4 * i + 3]));
+                        blk_flush(stage, f, [&](int r) -> uint8_t* {
+                            const long long to = __shfl_sync(0xffffffffu, live ? prow : -1ll, r);
+                            return to < 0 ? nullptr : reinterpret_cast<uint8_t*>(p.o_parts + to * 128 + t * 64 + c * 32 + h * 16);
+                        });
+                    }
                 }
             }
             if (live && t == 0) {
@@ -744,8 +743,6 @@ attn_blk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar_done);
-            ok = mbar_wait(bar_done, x_it & 1, s_abort, 636);      // (both accumulators and the statistics are read)
-            if (!ok) break;
             ++x_it;
         }
     }

@@ -174,8 +174,8 @@ vpp_status block_plan(const vpp_chunk_attn_args* a, int32_t topk, BlockPlan* b) 
     const size_t lists = static_cast<size_t>(tiles * H) * pages;
     b->items = align_up(sizeof(vpp::WorkHeader), 256);
     b->pages = align_up(b->items + sizeof(vpp::BlkItem) * static_cast<size_t>(tiles * H), 256);
-    b->masks = align_up(b->pages + sizeof(int2) * lists, 256);
-    b->o_parts = b->lse_parts = b->total = align_up(b->masks + sizeof(uint32_t) * lists * b->words, 256);
+    b->masks = align_up(b->pages + sizeof(int32_t) * lists, 256);
+    b->o_parts = b->lse_parts = b->total = align_up(b->masks + sizeof(uint2) * lists * b->words, 256);
     if (s > 1) {
         const size_t rows = static_cast<size_t>(s) * T * a->num_q_heads;
         b->lse_parts = align_up(b->o_parts + rows * 128 * sizeof(float), 256);
@@ -459,8 +459,8 @@ vpp_status vpp_block_attn_fwd(const vpp_chunk_attn_args* a, const int32_t* block
     lp.max_pages = b.max_pages;
     lp.header = reinterpret_cast<vpp::WorkHeader*>(ws);
     lp.items = reinterpret_cast<vpp::BlkItem*>(ws + b.items);
-    lp.pages = reinterpret_cast<int2*>(ws + b.pages);
-    lp.masks = reinterpret_cast<uint32_t*>(ws + b.masks);
+    lp.pages = reinterpret_cast<int32_t*>(ws + b.pages);
+    lp.masks = reinterpret_cast<uint2*>(ws + b.masks);
     lp.status = a->status;
     const size_t lens = 2 * sizeof(int32_t) * (static_cast<size_t>(a->num_reqs) + 1);
     cudaError_t ce = cudaFuncSetAttribute(vpp::block_lists_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lens));
