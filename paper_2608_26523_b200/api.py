@@ -395,10 +395,13 @@ def vpp_block_means(k_cache, k_means, block_table, prefix_len, chunk_len, block_
     _check(load_library().vpp_block_means(ctypes.byref(a), stream))
 
 
-def vpp_block_select_workspace_size(total_q, num_reqs, num_q_heads, num_kv_heads, block_size, max_seq_len):
-    a = BlockSelectArgs(num_reqs=int(num_reqs), block_size=int(block_size), total_q=int(total_q), max_seq_len=int(max_seq_len),
-                        num_q_heads=int(num_q_heads), num_kv_heads=int(num_kv_heads), head_dim=128, topk=1, num_last=1)
-    return int(load_library().vpp_block_select_workspace_size(ctypes.byref(a)))
+def vpp_block_select_workspace_size(total_q, num_reqs, num_q_heads, num_kv_heads, block_size, max_seq_len, topk=None):
+    """Bytes of workspace of vpp_block_select; topk None: enough for every topk."""
+    def size(k):
+        a = BlockSelectArgs(num_reqs=int(num_reqs), block_size=int(block_size), total_q=int(total_q), max_seq_len=int(max_seq_len),
+                            num_q_heads=int(num_q_heads), num_kv_heads=int(num_kv_heads), head_dim=128, topk=k, num_first=0, num_last=1)
+        return int(load_library().vpp_block_select_workspace_size(ctypes.byref(a)))
+    return size(int(topk)) if topk is not None else max(size(k) for k in (1, 64, 128, 256))
 
 
 def vpp_block_select(q, k_means, block_table, prefix_len, chunk_len, block_size, max_seq_len, indices, workspace, num_first=0, num_last=1,

@@ -80,24 +80,8 @@ __global__ void __launch_bounds__(kBlkListThreads) block_lists_kernel(const BlkL
         }
         return;
     }
-    if (warp == 0) {
-        int carry = 0;
-        for (int b = 0; b < p.num_reqs; b += 32) {
-            const int r = b + lane;
-            const int n = r < p.num_reqs ? (cu[r + 1] - cu[r] + p.tile_tokens - 1) / p.tile_tokens : 0;
-            int x = n;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int y = __shfl_up_sync(0xffffffffu, x, o);
-                if (lane >= o) x += y;
-            }
-            if (r < p.num_reqs) first_tile[r] = carry + x - n;
-            carry += __shfl_sync(0xffffffffu, x, 31);
-        }
-        if (lane == 0) first_tile[p.num_reqs] = carry;
-    }
     if (tid == 0) s_bad = 0;
-    __syncthreads();
+    block_scan<kBlkListThreads>(p.num_reqs, 0x7fffffffu, first_tile, false, [&](int r, bool&) { return (cu[r + 1] - cu[r] + p.tile_tokens - 1) / p.tile_tokens; });
     const int tiles = first_tile[p.num_reqs];
     if (blockIdx.x == 0 && tid == 0) {
         *p.header = WorkHeader{tiles, 0, 0, 0, 0, 0, 0, 0, {}};

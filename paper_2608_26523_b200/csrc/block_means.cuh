@@ -33,10 +33,10 @@ struct MeansParams {
 
 // The first work_blocks blocks form means; the block after them, if there is one, writes the status.
 __global__ void __launch_bounds__(kMeansThreads) block_means_kernel(const MeansParams p, const int work_blocks) {
-    extern __shared__ int32_t cu[];   // pages completed before request r; cu[num_reqs] = all
+    extern __shared__ int32_t cu[];   // rows before request r, cu[num_reqs] = all; then pages completed before it, the same
     __shared__ float s_sum[kMeansGroups][16][9];     // (a lane's eight features; 9: no bank conflicts)
-    __shared__ int s_wsum[kMeansThreads / 32];
-    const int tid = threadIdx.x, lane = tid & 31;
+    int32_t* const done = cu + p.num_reqs + 1;
+    const int tid = threadIdx.x;
     pdl_launch_dependents();
     pdl_wait();
     const bool ok = scan_lengths<kMeansThreads>(p.prefix_len, p.chunk_len, p.num_reqs, p.capacity, p.total_q, cu);
@@ -45,38 +45,14 @@ __global__ void __launch_bounds__(kMeansThreads) block_means_kernel(const MeansP
         if (checks && tid == 0) *p.status = 1 /* VPP_DEV_BAD_LENGTHS */;
         return;
     }
-    // chunk lengths become counts of completed pages, in place
-    int carry = 0;
-    for (int base = 0; base < p.num_reqs; base += kMeansThreads) {
-        const int r = base + tid;
-        int n = 0;
-        if (r < p.num_reqs) {
-            const int pre = p.prefix_len[r];
-            n = ((pre + (cu[r + 1] - cu[r])) >> p.block_shift) - (pre >> p.block_shift);
-        }
-        int x = n;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int y = __shfl_up_sync(0xffffffffu, x, o);
-            if (lane >= o) x += y;
-        }
-        if (lane == 31) s_wsum[tid >> 5] = x;
-        __syncthreads();              // (cu[r + 1] of the last thread is the next round's cu[r]: all have read)
-        int before = carry, all = 0;
-        for (int w = 0; w < kMeansThreads / 32; ++w) {
-            if (w < (tid >> 5)) before += s_wsum[w];
-            all += s_wsum[w];
-        }
-        if (r < p.num_reqs) cu[r] = before + x - n;
-        carry += all;
-        __syncthreads();
-    }
-    if (tid == 0) cu[p.num_reqs] = carry;
-    __syncthreads();
-    const long long pages = carry;
+    block_scan<kMeansThreads>(p.num_reqs, 0x7fffffffu, done, false, [&](int r, bool&) {
+        const int pre = p.prefix_len[r];
+        return ((pre + (cu[r + 1] - cu[r])) >> p.block_shift) - (pre >> p.block_shift);
+    });
+    const long long pages = done[p.num_reqs];
     auto page_of = [&](int i) {        // physical page of the i-th completed one
-        const int r = request_of(cu, p.num_reqs, i);
-        return __ldg(p.block_table + static_cast<long long>(r) * p.max_blocks_per_req + (p.prefix_len[r] >> p.block_shift) + (i - cu[r]));
+        const int r = request_of(done, p.num_reqs, i);
+        return __ldg(p.block_table + static_cast<long long>(r) * p.max_blocks_per_req + (p.prefix_len[r] >> p.block_shift) + (i - done[r]));
     };
     if (checks) {
         bool bad = false;

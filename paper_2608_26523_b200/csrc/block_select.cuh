@@ -8,15 +8,17 @@
 // The selection is that of exact arithmetic.  Scores are formed in 32 bits with a bound on their error, and where two pages near
 // the border are closer than the bound allows to tell, theirs are formed again in 64 bits (products of bf16 are exact there).
 //
-// Two kernels a slab of tokens (as many as have scores of kSelectSlabBytes together, so that these stay in the L2):
-//  * block_scores_kernel: an item is (up to 128 tokens of one request, kv-head, a run of pages).  The group's queries are
+// Two kernels a slab of tokens (one slab unless their candidates take more than kSelectSlabBytes):
+//  * block_filter_kernel: an item is (up to 128 tokens of one request, kv-head, a run of pages).  The group's queries are
 //    summed first, in 32 bits, and the sum split in two bf16 (hi + rest: 16 bits of it), so that the tensor cores do 2 / group
-//    of the work of all q-heads; scores of 128 tokens x 128 pages are one accumulator.  Reading q bounds it (134 MB of 8192 tokens of 64 heads are
-//    21 us; the products 8 us at the matrix rate).  Items of up to kSelectFew tokens -- decode rows -- take the dot products in
-//    registers instead, half a warp a page: there reading the means is all.
-//  * block_pick_kernel: a warp a (token, kv-head).  The need-th largest of 128 group maxima bounds the border from below; what
-//    is not below it by more than the error bound (a few more than needed) is gathered in index order, ranked, and the
-//    border settled.
+//    of the work of all q-heads; scores of 128 tokens x 128 pages are one accumulator.  They are formed twice: the first time the maxima of groups
+//    of pages are kept, whose need-th largest bounds a token's border from below; the second time what is not below that by more than the error
+//    bound -- a few more pages than needed -- is written down, a thread a token and half of the pages.  Reading q bounds it (134 MB of
+//    8192 tokens of 64 heads are 21 us; the products twice 4).  (All scores written down once, 4.6 KB a token and kv-head, and picked
+//    from there: 8192 tokens of 64/4 heads with 1152 pages 420 us.)
+//    Items of up to kSelectFew tokens -- decode rows -- take the dot products in registers, half a warp a page, and keep the scores in shared
+//    memory: there reading the means is all.
+//  * block_pick_kernel: a warp a (token, kv-head) ranks the candidates and settles the border.
 #pragma once
 #include <cstdint>
 
@@ -29,11 +31,19 @@ namespace vpp {
 constexpr int kSelectThreads = 256;
 constexpr int kSelectTile = 128;              // tokens of an item, pages of a step
 constexpr int kSelectFew = 4;
-constexpr int kSelectSlabBytes = 64 << 20;
+constexpr int kSelectSlabBytes = 128 << 20;
 constexpr int kSelectMaxTopk = 256;
+constexpr int kSelectMaxRun = 4096;           // pages of an item: scores of kSelectFew tokens are kept in shared memory
 constexpr int kSelectA = 2 * 2 * kSelectTile * 128;   // two bf16 parts of 128 x 128, two 64-feature slabs each
 constexpr int kSelectB = 2 * kSelectTile * 128;
-constexpr int kSelectSmem = kSelectA + kSelectB + 1024 /* alignment */ + 1024 /* barrier, bounds */;
+constexpr int kSelectSmem = kSelectA + kSelectB + 1024 /* alignment */ + 2048 /* barrier, borders */;
+static_assert(kSelectFew * kSelectMaxRun * 4 <= kSelectA, "scores of few tokens");
+
+// A page that may be among a token's best.
+struct __align__(8) SelectCandidate {
+    float score;
+    int32_t page;
+};
 
 struct SelectParams {
     const uint8_t* q;             // [total_q, Hq, 128] bf16
@@ -47,9 +57,12 @@ struct SelectParams {
     int topk, num_first, num_last;
     int row0, row1;               // this slab's tokens
     int run_pages, runs;          // pages of an item (a multiple of 128), items along a row
-    int row_pages;                // floats of a row of scores
-    float* scores;                // [row1 - row0, Hkv, row_pages]
+    int group_pages;              // pages of a group of which the maximum is kept (8, 4, 2, 1)
+    int cap;                      // candidates of half an item's pages, at most
+    SelectCandidate* found;       // [row1 - row0, Hkv, runs, 2, cap]
+    int32_t* counts;              // [row1 - row0, Hkv, runs, 2] (past cap: more than fit)
     float* bounds;                // [row1 - row0, Hkv, runs]: error bound of the row's scores of a run
+    float* maxima;                // [items, 128, run_pages / group_pages]
     int32_t* bad;                 // one word an item of the slab
     int items;
     int32_t* indices;             // [total_q, Hkv, topk]
@@ -80,12 +93,47 @@ __device__ __forceinline__ float select_bound(float a, uint32_t max_bits) {
     return a * m * 6.103515625e-5f + 1e-35f;
 }
 
-__device__ __forceinline__ void st_v8(float* p, const uint32_t* r) {
-    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]),
-                 "r"(r[6]), "r"(r[7]) : "memory");
+// Unsigned integers in the order of floats; NaN below everything.
+__device__ __forceinline__ uint32_t order_key(float f) {
+    if (!(f == f)) return 0;
+    const uint32_t u = __float_as_uint(f + 0.f);          // (-0 becomes 0)
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
+
+// A value that at least `need` of n numbers reach, and not many more: the need-th largest of 32 * kKeys maxima over value(i), i = lane + 32 k, by a warp.
+// -inf where there are fewer maxima.
+template <int kKeys, typename Value>
+__device__ __forceinline__ float border_below(int n, int need, Value value) {
+    const int lane = threadIdx.x & 31;
+    float mx[kKeys];
+#pragma unroll
+    for (int k = 0; k < kKeys; ++k) mx[k] = -INFINITY;
+    for (int i = lane; i < n; i += 32 * kKeys) {
+#pragma unroll
+        for (int k = 0; k < kKeys; ++k)
+            if (i + 32 * k < n) mx[k] = fmaxf(mx[k], value(i + 32 * k));
+    }
+    uint32_t key[kKeys], t = 0;
+#pragma unroll
+    for (int k = 0; k < kKeys; ++k) key[k] = order_key(mx[k]);
+    for (int b = 31; b >= 8; --b) {              // (a little below will do)
+        const uint32_t c = t | (1u << b);
+        int k = 0;
+#pragma unroll
+        for (int e = 0; e < kKeys; ++e) k += key[e] >= c;
+        const int all = static_cast<int>(__reduce_add_sync(0xffffffffu, k));
+        if (all >= need) t = c;
+        if (all == need) break;
+    }
+    return t < 0x00800000u ? -INFINITY : key_value(t);      // (maxima of nothing)
+}
+template <typename Value>
+__device__ __forceinline__ float border_of(int n, int need, Value value) {
+    return need <= 64 ? border_below<8>(n, need, value) : border_below<16>(n, need, value);
 }
 
-__global__ void __launch_bounds__(kSelectThreads) block_scores_kernel(const SelectParams p) {
+__global__ void __launch_bounds__(kSelectThreads, 2) block_filter_kernel(const SelectParams p) {
     extern __shared__ uint8_t smem_raw[];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -98,8 +146,9 @@ __global__ void __launch_bounds__(kSelectThreads) block_scores_kernel(const Sele
     volatile uint32_t* const s_tmem = reinterpret_cast<volatile uint32_t*>(sX + 12);
     uint32_t* const s_max = reinterpret_cast<uint32_t*>(sX + 16);
     int* const s_badp = reinterpret_cast<int*>(sX + 20);
-    float* const s_a = reinterpret_cast<float*>(sX + 32);          // [128]
-    int32_t* const cu = reinterpret_cast<int32_t*>(sX + 1024);     // [num_reqs + 1], then tile counts [num_reqs + 1]
+    float* const s_a = reinterpret_cast<float*>(sX + 32);              // [128] what a bound is made of
+    float* const s_floor = reinterpret_cast<float*>(sX + 32 + 512);    // [128] lowest score of a candidate
+    int32_t* const cu = reinterpret_cast<int32_t*>(sX + 2048);         // [num_reqs + 1], then tile counts [num_reqs + 1]
     int32_t* const first_tile = cu + p.num_reqs + 1;
 
     pdl_launch_dependents();
@@ -116,23 +165,6 @@ __global__ void __launch_bounds__(kSelectThreads) block_scores_kernel(const Sele
         const int n = min(cu[r + 1], p.row1) - lo;
         return n > 0 ? n : 0;
     };
-    if (warp == 0) {
-        int carry = 0;
-        for (int b = 0; b < p.num_reqs; b += 32) {
-            const int r = b + lane;
-            int lo, n = 0;
-            if (r < p.num_reqs) n = (rows_of(r, lo) + kSelectTile - 1) / kSelectTile;
-            int x = n;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int y = __shfl_up_sync(0xffffffffu, x, o);
-                if (lane >= o) x += y;
-            }
-            if (r < p.num_reqs) first_tile[r] = carry + x - n;
-            carry += __shfl_sync(0xffffffffu, x, 31);
-        }
-        if (lane == 0) first_tile[p.num_reqs] = carry;
-    }
     if (tid == 0) {
         *s_abort = 0;
         *s_max = 0;
@@ -140,7 +172,10 @@ __global__ void __launch_bounds__(kSelectThreads) block_scores_kernel(const Sele
         mbar_init(bar, 1);
         fence_mbar_init();
     }
-    __syncthreads();
+    block_scan<kSelectThreads>(p.num_reqs, 0x7fffffffu, first_tile, false, [&](int r, bool&) {
+        int lo;
+        return (rows_of(r, lo) + kSelectTile - 1) / kSelectTile;
+    });
     const int run = item % p.runs, tg = item / p.runs, g = tg % p.num_kv_heads, tile = tg / p.num_kv_heads;
     if (tile >= first_tile[p.num_reqs]) {
         if (tid == 0) p.bad[item] = 0;
@@ -154,21 +189,27 @@ __global__ void __launch_bounds__(kSelectThreads) block_scores_kernel(const Sele
     const int pos0 = p.prefix_len[r] + (row - cu[r]);
     const int end = select_end(p, (pos0 + n - 1) >> p.block_shift);      // of the tile's last token
     // a page run that nobody needs: below the first candidate, past the last, or no token has more pages than it may list
-    const int page0 = run * p.run_pages, page1 = min(page0 + p.run_pages, end);
-    if (page1 <= max(page0, p.num_first) || ((pos0 + n - 1) >> p.block_shift) + 1 <= p.topk) {
+    const int page0 = run * p.run_pages, page1 = min(page0 + p.run_pages, end), begin = max(page0, p.num_first);
+    if (page1 <= begin || ((pos0 + n - 1) >> p.block_shift) + 1 <= p.topk) {
         if (tid == 0) p.bad[item] = 0;
         return;
     }
-    const int G = p.num_q_heads / p.num_kv_heads;
+    const int G = p.num_q_heads / p.num_kv_heads, need = p.topk - p.num_first - p.num_last;
     const int32_t* const table = p.block_table + static_cast<long long>(r) * p.max_blocks_per_req;
     const uint8_t* const q0 = p.q + (static_cast<long long>(row) * p.num_q_heads + g * G) * 256;
-    const long long score_row0 = static_cast<long long>(row - p.row0) * p.num_kv_heads + g;      // of the tile's first token; tokens are Hkv rows apart
+    // of token t of the tile: candidates of this run (one past the last), and where its lists are
+    auto end_of = [&](int t) {
+        const int own = (pos0 + t) >> p.block_shift;
+        return own + 1 <= p.topk ? 0 : min(page1, select_end(p, own));
+    };
+    auto list_of = [&](int t) { return (static_cast<long long>(row - p.row0 + t) * p.num_kv_heads + g) * p.runs + run; };
     const int v = tid & 15;
     bool bad = false;
     uint32_t top = 0;
 
     if (n <= kSelectFew) {
         // ---- a few tokens: half a warp a page ----
+        float* const s_score = reinterpret_cast<float*>(sA);       // [kSelectFew][run_pages]
         float s[kSelectFew][8], a[kSelectFew];
 #pragma unroll
         for (int t = 0; t < kSelectFew; ++t) {
@@ -192,24 +233,28 @@ __global__ void __launch_bounds__(kSelectThreads) block_scores_kernel(const Sele
 #pragma unroll
             for (int o = 8; o > 0; o >>= 1) a[t] += __shfl_xor_sync(0xffffffffu, a[t], o);
         }
-        constexpr int kDeep = 4;
+        constexpr int kDeep = 8, kStep = kDeep * (kSelectThreads / 16);
         const int half = tid >> 4;
-        for (int j0 = page0; j0 < page1; j0 += kDeep * (kSelectThreads / 16)) {
-            uint4 x[kDeep];
-            int e[kDeep];
+        int e[kDeep];
+        auto look = [&](int j0) {
 #pragma unroll
             for (int i = 0; i < kDeep; ++i) {
                 const int j = j0 + i * (kSelectThreads / 16) + half;
                 e[i] = j < page1 ? __ldg(table + j) : 0;
             }
+        };
+        look(page0);
+        for (int j0 = page0; j0 < page1; j0 += kStep) {
+            uint4 x[kDeep];
 #pragma unroll
             for (int i = 0; i < kDeep; ++i) {
                 const int j = j0 + i * (kSelectThreads / 16) + half;
                 const bool fine = e[i] >= 0 && e[i] < p.num_blocks;
                 bad |= !fine;
                 x[i] = make_uint4(0, 0, 0, 0);
-                if (j < page1 && j >= p.num_first && fine) x[i] = ld_once(p.means + (static_cast<long long>(e[i]) * p.num_kv_heads + g) * 256 + v * 16);
+                if (j < page1 && j >= begin && fine) x[i] = ld_once(p.means + (static_cast<long long>(e[i]) * p.num_kv_heads + g) * 256 + v * 16);
             }
+            look(j0 + kStep);
 #pragma unroll
             for (int i = 0; i < kDeep; ++i) {
                 const int j = j0 + i * (kSelectThreads / 16) + half;
@@ -226,19 +271,42 @@ __global__ void __launch_bounds__(kSelectThreads) block_scores_kernel(const Sele
                     }
 #pragma unroll
                     for (int o = 8; o > 0; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
-                    if (v == 0 && j < page1) p.scores[(score_row0 + static_cast<long long>(t) * p.num_kv_heads) * p.row_pages + j] = d;
+                    if (v == 0 && j < page1) s_score[t * p.run_pages + j - page0] = d;
                 }
             }
         }
-        atomicMax(s_max, top);
+        top = __reduce_max_sync(0xffffffffu, top);
+        if (lane == 0) atomicMax(s_max, top);
         if (bad) *s_badp = 1;
         __syncthreads();
-        if (tid < n) {
+        if (warp < n) {
             float at = a[0];
 #pragma unroll
             for (int t = 1; t < kSelectFew; ++t)
-                if (tid == t) at = a[t];
-            p.bounds[(score_row0 + static_cast<long long>(tid) * p.num_kv_heads) * p.runs + run] = select_bound(at, *s_max);
+                if (warp == t) at = a[t];
+            const float bound = select_bound(at, *s_max);
+            const int stop = end_of(warp);
+            const long long list = list_of(warp);
+            const float* const mine = s_score + warp * p.run_pages - page0;
+            if (lane == 0) p.bounds[list] = bound;
+            int m = 0;
+            if (bound > 0.f && bound < INFINITY && stop > begin) {
+                const float floor = stop - begin <= p.cap ? -INFINITY : border_of(stop - begin, need, [&](int i) { return mine[begin + i]; }) - 2.f * bound;
+                SelectCandidate* const found = p.found + list * 2 * p.cap;
+                for (int j0 = begin; j0 < stop; j0 += 32) {
+                    const int j = j0 + lane;
+                    const float x = j < stop ? mine[j] : 0.f;
+                    const bool take = j < stop && x >= floor;
+                    const uint32_t b = __ballot_sync(0xffffffffu, take);
+                    const int at_m = m + __popc(b & ((1u << lane) - 1));
+                    if (take && at_m < p.cap) found[at_m] = SelectCandidate{x, j};
+                    m += __popc(b);
+                }
+            }
+            if (lane == 0) {
+                p.counts[list * 2] = m;
+                p.counts[list * 2 + 1] = 0;
+            }
         }
         if (tid == 0) p.bad[item] = *s_badp ? 2 /* VPP_DEV_BAD_BLOCK */ : 0;
         return;
@@ -250,22 +318,25 @@ __global__ void __launch_bounds__(kSelectThreads) block_scores_kernel(const Sele
         tmem_relinquish();
     }
     uint4 x[8];
-    auto fetch = [&](int j0) {        // 128 pages' means: the thread's eight vectors, of rows tid / 16 + 16 i
-        int e[8];
+    int e[8];
+    auto look = [&](int j0) {         // pages of the thread's eight vectors, rows tid / 16 + 16 i of the step
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int j = j0 + (tid >> 4) + 16 * i;
             e[i] = j < page1 ? __ldg(table + j) : 0;
         }
+    };
+    auto fetch = [&](int j0) {        // their means
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int j = j0 + (tid >> 4) + 16 * i;
             const bool fine = e[i] >= 0 && e[i] < p.num_blocks;
             bad |= !fine;
             x[i] = make_uint4(0, 0, 0, 0);        // (pages that are taken anyway count as 0: what theirs hold must not widen the bound)
-            if (j < page1 && j >= p.num_first && fine) x[i] = ld_once(p.means + (static_cast<long long>(e[i]) * p.num_kv_heads + g) * 256 + v * 16);
+            if (j < page1 && j >= begin && fine) x[i] = ld_once(p.means + (static_cast<long long>(e[i]) * p.num_kv_heads + g) * 256 + v * 16);
         }
     };
+    look(page0);
     for (int t = tid >> 4; t < n; t += kSelectThreads / 16) {
         float s[8] = {}, a = 0.f;
         const uint8_t* src = q0 + static_cast<long long>(t) * p.num_q_heads * 256 + v * 16;
@@ -274,10 +345,10 @@ __global__ void __launch_bounds__(kSelectThreads) block_scores_kernel(const Sele
             const uint4 y = ld_once(src + h * 256);
             const uint32_t w[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                s[2 * e] += bf16_lo(w[e]);
-                s[2 * e + 1] += bf16_hi(w[e]);
-                a += fabsf(bf16_lo(w[e])) + fabsf(bf16_hi(w[e]));
+            for (int k = 0; k < 4; ++k) {
+                s[2 * k] += bf16_lo(w[k]);
+                s[2 * k + 1] += bf16_hi(w[k]);
+                a += fabsf(bf16_lo(w[k])) + fabsf(bf16_hi(w[k]));
             }
         }
         const unsigned half_mask = 0xffffu << (lane & 16);        // (the other half's token may not exist)
@@ -285,9 +356,9 @@ __global__ void __launch_bounds__(kSelectThreads) block_scores_kernel(const Sele
         for (int o = 8; o > 0; o >>= 1) a += __shfl_xor_sync(half_mask, a, o);
         uint32_t hi[4], rest[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            hi[e] = pack_bf16x2(s[2 * e], s[2 * e + 1]);
-            rest[e] = pack_bf16x2(s[2 * e] - bf16_lo(hi[e]), s[2 * e + 1] - bf16_hi(hi[e]));
+        for (int k = 0; k < 4; ++k) {
+            hi[k] = pack_bf16x2(s[2 * k], s[2 * k + 1]);
+            rest[k] = pack_bf16x2(s[2 * k] - bf16_lo(hi[k]), s[2 * k + 1] - bf16_hi(hi[k]));
         }
         uint8_t* const to = sA + (v >> 3) * (kSelectTile * 128) + t * 128 + (((v & 7) ^ (t & 7)) << 4);
         *reinterpret_cast<uint4*>(to) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
@@ -300,52 +371,124 @@ __global__ void __launch_bounds__(kSelectThreads) block_scores_kernel(const Sele
     tc_fence_after();
     const uint32_t tmem = *s_tmem;
     constexpr uint32_t kIdesc = idesc_bf16(kSelectTile, kSelectTile, false, false), kHi = desc_hi_sw128(1024);
-    const int my_row = (warp & 3) * 32 + lane, col0 = (warp >> 2) * 64;
-    float* const out = p.scores + (score_row0 + static_cast<long long>(my_row) * p.num_kv_heads) * p.row_pages;
+    const int my_row = (warp & 3) * 32 + lane, half = warp >> 2;
+    const int stop = my_row < n ? end_of(my_row) : 0;
+    const int gp = p.group_pages, row_groups = p.run_pages / gp;
+    float* const my_maxima = p.maxima + (static_cast<long long>(item) * kSelectTile + my_row) * row_groups;
+    // no more candidates than fit: no border is needed
+    const bool filter = page1 - begin > p.cap;
     uint32_t phase = 0;
     bool alive = true;
-    for (int j0 = page0; j0 < page1; j0 += kSelectTile) {
+    float floor = -INFINITY;
+    int m = 0;
+    SelectCandidate* const found = p.found + (list_of(my_row) * 2 + half) * p.cap;
+    for (int pass = filter ? 0 : 1; pass < 2 && alive; ++pass) {
+        for (int j0 = page0; j0 < page1; j0 += kSelectTile) {
+            const bool more = j0 + kSelectTile < page1;
+            if (more || pass == 0) look(more ? j0 + kSelectTile : page0);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int t = (tid >> 4) + 16 * i;
-            top = abs_max(top, x[i]);
-            *reinterpret_cast<uint4*>(sB + (v >> 3) * (kSelectTile * 128) + t * 128 + (((v & 7) ^ (t & 7)) << 4)) = x[i];
-        }
-        fence_proxy_async_smem();
-        __syncthreads();              // (operands in place; the last step's scores have left tensor memory)
-        if (tid == 0) {
+            for (int i = 0; i < 8; ++i) {
+                const int t = (tid >> 4) + 16 * i;
+                top = abs_max(top, x[i]);
+                *reinterpret_cast<uint4*>(sB + (v >> 3) * (kSelectTile * 128) + t * 128 + (((v & 7) ^ (t & 7)) << 4)) = x[i];
+            }
+            fence_proxy_async_smem();
+            __syncthreads();              // (operands in place; the last step's scores have left tensor memory)
+            if (tid == 0) {
+                tc_fence_after();
+                const uint32_t a0 = desc_lo_sw128(base, 16), b0 = desc_lo_sw128(base + kSelectA, 16);
+#pragma unroll
+                for (int k = 0; k < 16; ++k) {
+                    const uint32_t at = (((k >> 2) & 1) * (kSelectTile * 128) + (k & 3) * 32) >> 4;
+                    mma_ss_lhh(tmem, a0 + (k >> 3) * (kSelectA / 2 >> 4) + at, kHi, b0 + at, kHi, kIdesc, k > 0);
+                }
+                tc_commit(bar);
+            }
+            if (more || pass == 0) fetch(more ? j0 + kSelectTile : page0);
+            alive = __syncthreads_and(mbar_wait(bar, phase, s_abort, 501));
+            if (!alive) break;
+            phase ^= 1;
             tc_fence_after();
-            const uint32_t a0 = desc_lo_sw128(base, 16), b0 = desc_lo_sw128(base + kSelectA, 16);
 #pragma unroll
-            for (int k = 0; k < 16; ++k) {
-                const uint32_t at = (((k >> 2) & 1) * (kSelectTile * 128) + (k & 3) * 32) >> 4;
-                mma_ss_lhh(tmem, a0 + (k >> 3) * (kSelectA / 2 >> 4) + at, kHi, b0 + at, kHi, kIdesc, k > 0);
+            for (int c = 0; c < 2; ++c) {
+                uint32_t s[32];
+                tmem_ld32(tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + half * 64 + c * 32, s);
+                tc_wait_ld(s);
+                const int j = j0 + half * 64 + c * 32;      // page of the first column
+                if (j >= page1) continue;
+                if (j < begin || __any_sync(0xffffffffu, j + 32 > stop)) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i)
+                        if (j + i < begin || j + i >= stop) s[i] = 0xff800000u;   // -inf
+                }
+                if (pass == 0) {
+                    if (my_row < n) {
+                        float4* const to = reinterpret_cast<float4*>(my_maxima + (j - page0) / gp);
+                        auto at = [&](int i) { return __uint_as_float(s[i]); };
+                        auto two = [&](int i) { return fmaxf(at(2 * i), at(2 * i + 1)); };
+                        auto four = [&](int i) { return fmax3(at(4 * i), at(4 * i + 1), fmaxf(at(4 * i + 2), at(4 * i + 3))); };
+                        auto eight = [&](int i) { return fmaxf(four(2 * i), four(2 * i + 1)); };
+                        if (gp == 8) {
+                            to[0] = make_float4(eight(0), eight(1), eight(2), eight(3));
+                        } else if (gp == 4) {
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) to[i] = make_float4(four(4 * i), four(4 * i + 1), four(4 * i + 2), four(4 * i + 3));
+                        } else if (gp == 2) {
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) to[i] = make_float4(two(4 * i), two(4 * i + 1), two(4 * i + 2), two(4 * i + 3));
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) to[i] = make_float4(at(4 * i), at(4 * i + 1), at(4 * i + 2), at(4 * i + 3));
+                        }
+                    }
+                } else {
+                    // (a page that is not a candidate is -inf: with a border of -inf it must be told by its number)
+                    const int last = stop - j, lead = begin - j;
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) {
+                        const float y = __uint_as_float(s[i]);
+                        if (y >= floor && i < last && i >= lead) {
+                            if (m < p.cap) found[m] = SelectCandidate{y, j + i};
+                            ++m;
+                        }
+                    }
+                }
+                __syncwarp();
             }
-            tc_commit(bar);
+            tc_fence_before();
         }
-        if (j0 + kSelectTile < page1) fetch(j0 + kSelectTile);
-        alive = mbar_wait(bar, phase, s_abort, 501);
-        if (!__syncthreads_and(alive)) break;
-        phase ^= 1;
-        tc_fence_after();
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-            uint32_t s[32];
-            tmem_ld32(tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + col0 + c * 32, s);
-            tc_wait_ld();
-            if (my_row < n) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) st_v8(out + j0 + col0 + c * 32 + i * 8, s + i * 8);
+        if (!alive || pass == 1) continue;
+        // ---- the borders ----
+        const uint32_t warp_top = __reduce_max_sync(0xffffffffu, top);
+        if (lane == 0) atomicMax(s_max, warp_top);
+        __syncthreads();
+        const int lead_group = (begin - page0) / gp;
+        for (int t = warp; t < n; t += kSelectThreads / 32) {
+            const int stop_t = end_of(t);
+            float f = INFINITY;          // (lists without choice, or bounds that say nothing: no candidates)
+            const float bound = select_bound(s_a[t], *s_max);
+            if (stop_t > begin && bound > 0.f && bound < INFINITY) {
+                f = -INFINITY;
+                if (stop_t - begin > p.cap) {
+                    const float* const mx = p.maxima + (static_cast<long long>(item) * kSelectTile + t) * row_groups + lead_group;
+                    f = border_of((stop_t - page0 + gp - 1) / gp - lead_group, need, [&](int i) { return mx[i]; }) - 2.f * bound;
+                }
             }
+            if (lane == 0) s_floor[t] = f;
         }
-        tc_fence_before();
+        __syncthreads();
+        if (my_row < n) floor = s_floor[my_row];
     }
-    atomicMax(s_max, top);
+    const uint32_t warp_top = __reduce_max_sync(0xffffffffu, top);
+    if (lane == 0) atomicMax(s_max, warp_top);
     if (bad) *s_badp = 1;
     if (*s_abort != 0)
         for (int i = 0; i < 64; ++i) __nanosleep(1000);  // let MMAs in flight drain
     __syncthreads();
-    if (tid < n) p.bounds[(score_row0 + static_cast<long long>(tid) * p.num_kv_heads) * p.runs + run] = select_bound(s_a[tid], *s_max);
+    if (my_row < n) {
+        p.counts[list_of(my_row) * 2 + half] = m;
+        if (half == 0) p.bounds[list_of(my_row)] = select_bound(s_a[my_row], *s_max);
+    }
     if (tid == 0) p.bad[item] = *s_abort != 0 ? 3 /* VPP_DEV_TIMEOUT */ : *s_badp ? 2 /* VPP_DEV_BAD_BLOCK */ : 0;
     if (warp == 0) tmem_dealloc(tmem, 128);
 }
@@ -355,22 +498,19 @@ __global__ void __launch_bounds__(kSelectThreads) block_scores_kernel(const Sele
 constexpr int kPickThreads = 256;
 constexpr int kPickGather = 512;              // entries a warp can gather
 constexpr int kPickClose = 128;               // entries near the border that it can settle at once
-static_assert(kSelectMaxTopk < kPickGather, "what is needed fits");
+static_assert(kSelectMaxTopk + kPickClose <= kPickGather, "what is needed fits");
 struct PickScratch {
-    double exact[kPickClose];
-    float score[kPickGather];
+    union {
+        struct {
+            double exact[kPickClose];         // of the near ones
+            float score[kPickGather];
+        };
+        double all[kPickGather];              // (pick_thorough)
+    };
     int32_t page[kPickGather];
     int32_t close[kPickClose];                // (entries of page / score)
 };
 constexpr int kPickSmem = static_cast<int>(sizeof(PickScratch)) * (kPickThreads / 32);
-
-// Unsigned integers in the order of floats; NaN below everything.
-__device__ __forceinline__ uint32_t order_key(float f) {
-    if (!(f == f)) return 0;
-    const uint32_t u = __float_as_uint(f + 0.f);          // (-0 becomes 0)
-    return u & 0x80000000u ? ~u : u | 0x80000000u;
-}
-__device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
 
 // A row's own inputs, for scores in 64 bits.
 struct PickRow {
@@ -409,26 +549,36 @@ __device__ __noinline__ void exact_scores(PickRow w, const int32_t* pages, const
     __syncwarp();
 }
 
-// Keeps of the m gathered entries (ascending pages, all that can be among the best) the `need` best: their pages move to the
-// front of s.page, in order.  delta: bound on the error of a score.  False: more of them are too close to tell than fit.
+// Keeps of the m gathered entries (all that can be among the best, in any order) the `need` best: their pages move to the front of
+// s.page, in any order.  delta > 0: bound on the error of a score.  False: more of them are too close to tell than fit.
 __device__ __forceinline__ bool pick_settle(PickScratch& s, const PickRow& w, int m, int need, float delta) {
     const int lane = threadIdx.x & 31;
     const uint32_t k0 = lane < m ? order_key(s.score[lane]) : 0, k1 = lane + 32 < m ? order_key(s.score[lane + 32]) : 0;
-    uint32_t border = 0;      // the need-th best score
+    // a key that `need` entries reach (or more, where the need-th and the next are equal), then the least of theirs: the need-th best score
+    uint32_t border = 0;
     for (int b = 31; b >= 0; --b) {
         const uint32_t c = border | (1u << b);
         int k = (k0 >= c) + (k1 >= c);
         for (int i = lane + 64; i < m; i += 32) k += order_key(s.score[i]) >= c;
-        if (static_cast<int>(__reduce_add_sync(0xffffffffu, k)) >= need) border = c;
+        const int all = static_cast<int>(__reduce_add_sync(0xffffffffu, k));
+        if (all >= need) border = c;
+        if (all == need) break;
     }
+    uint32_t least = 0xffffffffu;
+    if (k0 >= border && lane < m) least = k0;
+    if (k1 >= border && lane + 32 < m) least = min(least, k1);
+    for (int i = lane + 64; i < m; i += 32) {
+        const uint32_t k = order_key(s.score[i]);
+        if (k >= border) least = min(least, k);
+    }
+    border = __reduce_min_sync(0xffffffffu, least);
     const float v = key_value(border), hi = v + 2.f * delta, lo = v - 2.f * delta;
     // sure ones (above hi: their exact scores are above those of all but need - 1), and those too close to the border to tell
     int sure = 0, near_n = 0;
     for (int i0 = 0; i0 < m; i0 += 32) {
         const int i = i0 + lane;
         const float x = i < m ? s.score[i] : 0.f;
-        const uint32_t k = order_key(x);
-        const bool in = i < m && k > border && x > hi, near = i < m && !in && (k >= border || x >= lo);
+        const bool in = i < m && x > hi, near = i < m && !in && x >= lo;
         sure += __popc(__ballot_sync(0xffffffffu, in));
         const uint32_t b = __ballot_sync(0xffffffffu, near);
         const int at = near_n + __popc(b & ((1u << lane) - 1));
@@ -436,30 +586,29 @@ __device__ __forceinline__ bool pick_settle(PickScratch& s, const PickRow& w, in
         near_n += __popc(b);
     }
     const int left = need - sure;         // to be taken of the near ones: 1 .. near_n
-    const bool all = left == near_n, same = delta == 0.f;        // (same: all scores are exact, so the near ones are equal)
-    if (!all && !same) {
+    if (left != near_n) {
         if (near_n > kPickClose) return false;
         __syncwarp();
         exact_scores(w, s.page, s.close, 0, near_n, s.exact);
         // losers among the near ones get a page of -1
+        int lost = 0;
         for (int c = lane; c < near_n; c += 32) {
             const double d = s.exact[c];
+            const int page = s.page[s.close[c]];
             int before = 0;
-            for (int j = 0; j < near_n; ++j) before += s.exact[j] > d || (s.exact[j] == d && j < c);
-            if (before >= left) s.page[s.close[c]] = -1;
+            for (int j = 0; j < near_n; ++j) before += s.exact[j] > d || (s.exact[j] == d && s.page[s.close[j]] < page);
+            if (before >= left) lost |= 1 << (c >> 5);
         }
+        __syncwarp();                     // (all have read the pages)
+        for (int c = lane; c < near_n; c += 32)
+            if ((lost >> (c >> 5)) & 1) s.page[s.close[c]] = -1;
     }
     __syncwarp();
-    int kept = 0, seen = 0;
+    int kept = 0;
     for (int i0 = 0; i0 < m; i0 += 32) {
         const int i = i0 + lane;
-        const float x = i < m ? s.score[i] : 0.f;
         const int page = i < m ? s.page[i] : -1;
-        const uint32_t k = order_key(x);
-        const bool in = i < m && k > border && x > hi, near = i < m && !in && (k >= border || x >= lo);
-        const uint32_t b = __ballot_sync(0xffffffffu, near);
-        const bool take = in || (near && page >= 0 && (all || !same || seen + __popc(b & ((1u << lane) - 1)) < left));
-        seen += __popc(b);
+        const bool take = i < m && s.score[i] >= lo && page >= 0;
         const uint32_t t = __ballot_sync(0xffffffffu, take);      // (all have read their page)
         if (take) s.page[kept + __popc(t & ((1u << lane) - 1))] = page;
         kept += __popc(t);
@@ -468,137 +617,48 @@ __device__ __forceinline__ bool pick_settle(PickScratch& s, const PickRow& w, in
     return true;
 }
 
-// Entries of the row at or above `floor`, in order.  Returns their number; those past kPickGather are not stored.
-__device__ __forceinline__ int pick_gather(PickScratch& s, const float* row, int begin, int end, float floor) {
+// What the common path does not settle -- infinite or NaN scores, more candidates than fit (many pages that are (nearly) the same): all pages' scores in 64
+// bits, 128 at a time, each time joined with the best so far.
+__device__ __noinline__ void pick_thorough(PickScratch& s, PickRow w, int begin, int end, int need) {
     const int lane = threadIdx.x & 31;
-    int m = 0;
-    for (int j0 = begin; j0 < end; j0 += 32) {
-        const int j = j0 + lane;
-        const float x = j < end ? row[j] : 0.f;
-        const bool take = j < end && x >= floor;
-        const uint32_t b = __ballot_sync(0xffffffffu, take);
-        const int at = m + __popc(b & ((1u << lane) - 1));
-        if (take && at < kPickGather) {
-            s.score[at] = x;
-            s.page[at] = j;
-        }
-        m += __popc(b);
-    }
-    __syncwarp();
-    return m;
-}
-
-// What the common path does not settle: infinite or NaN scores, long lists of many pages, many pages that are (nearly) the same.
-__device__ __noinline__ void pick_thorough(PickScratch& s, PickRow w, float* row, int begin, int end, int need, float delta) {
-    const int lane = threadIdx.x & 31;
-    if (!(delta < INFINITY)) {
-        // scores anew: those of 64 bits, rounded
-        float big = 0.f;
-        for (int j0 = begin; j0 < end; j0 += kPickClose) {
-            const int n = min(kPickClose, end - j0);
-            exact_scores(w, nullptr, nullptr, j0, n, s.exact);
-            for (int c = lane; c < n; c += 32) {
-                const float x = static_cast<float>(s.exact[c]);
-                row[j0 + c] = x;
-                if (fabsf(x) < INFINITY) big = fmaxf(big, fabsf(x));
-            }
-            __syncwarp();
-        }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
-        delta = big * 1.1920929e-7f + 1e-44f;
-    }
-    uint32_t t = 0;       // the need-th best score
-    for (int b = 31; b >= 0; --b) {
-        const uint32_t c = t | (1u << b);
-        int k = 0;
-        for (int j = begin + lane; j < end; j += 32) k += order_key(row[j]) >= c;
-        if (static_cast<int>(__reduce_add_sync(0xffffffffu, k)) >= need) t = c;
-    }
-    const float floor = key_value(t) - 2.f * delta;       // (-inf stays, inf stays)
-    const int m = pick_gather(s, row, begin, end, floor);
-    if (m <= kPickGather && pick_settle(s, w, m, need, delta)) return;
-    // one after the other, in 64 bits
-    double last = INFINITY;
-    int last_page = -1;
-    for (int k = 0; k < need; ++k) {
-        double best = -INFINITY;
-        int best_page = INT32_MAX;
-        for (int j0 = begin; j0 < end; j0 += kPickClose) {
-            const int n = min(kPickClose, end - j0);
-            exact_scores(w, nullptr, nullptr, j0, n, s.exact);
-            for (int c = lane; c < n; c += 32) {
-                const double d = s.exact[c];
-                const int j = j0 + c;
-                if (d > last || (d == last && j <= last_page)) continue;      // taken already
-                if (best_page == INT32_MAX || d > best) {
-                    best = d;
-                    best_page = j;
-                }
-            }
-            __syncwarp();
-        }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-            const double d = __shfl_xor_sync(0xffffffffu, best, o);
-            const int j = __shfl_xor_sync(0xffffffffu, best_page, o);
-            if (j != INT32_MAX && (best_page == INT32_MAX || d > best || (d == best && j < best_page))) {
-                best = d;
-                best_page = j;
-            }
-        }
-        last = best;
-        last_page = best_page;
-        // kept ascending: those behind it move up by one
-        int before = 0;
-        for (int i = lane; i < k; i += 32) before += s.page[i] < best_page;
-        before = __reduce_add_sync(0xffffffffu, before);
-        for (int i0 = k / 32 * 32; i0 >= 0; i0 -= 32) {
-            const int i = i0 + lane;
-            const bool moves = i < k && i >= before;
-            const int page = moves ? s.page[i] : 0;
-            __syncwarp();
-            if (moves) s.page[i + 1] = page;
-            __syncwarp();
-        }
-        if (lane == 0) s.page[before] = best_page;
+    int best = 0;
+    for (int j0 = begin; j0 < end; j0 += kPickClose) {
+        const int n = min(kPickClose, end - j0), m = best + n;
+        exact_scores(w, nullptr, nullptr, j0, n, s.all + best);
+        for (int c = lane; c < n; c += 32) s.page[best + c] = j0 + c;
         __syncwarp();
-    }
-}
-
-// The best `need` of the pages [begin, end), end - begin > need > 0, into s.page, ascending.
-__device__ __forceinline__ void pick(PickScratch& s, const PickRow& w, float* row, int begin, int end, int need, float delta) {
-    if (delta < INFINITY && need <= 128) {       // (no infinite or NaN score)
-        const int lane = threadIdx.x & 31;
-        // the need-th largest of 128 maxima is not above the need-th largest of all
-        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-        int j = begin + lane;
-        for (; j + 96 < end; j += 128) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) mx[k] = fmaxf(mx[k], row[j + 32 * k]);
+        // ranks: better scores, then lower pages (the best so far are lower pages than the new ones, and in order of their pages)
+        uint32_t keep = 0;
+#pragma unroll 1
+        for (int k = 0; 32 * k < m; ++k) {
+            const int i = lane + 32 * k;
+            if (i >= m) continue;
+            const double d = s.all[i];
+            int before = 0;
+            for (int j = 0; j < m; ++j) before += s.all[j] > d || (s.all[j] == d && j < i);
+            if (before < need) keep |= 1u << k;
         }
-#pragma unroll
-        for (int k = 0; k < 3; ++k)
-            if (j + 32 * k < end) mx[k] = fmaxf(mx[k], row[j + 32 * k]);
-        uint32_t t = 0, key[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) key[k] = order_key(mx[k]);
-        for (int b = 31; b >= 10; --b) {         // (a little below will do)
-            const uint32_t c = t | (1u << b);
-            int k = 0;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) k += key[e] >= c;
-            if (static_cast<int>(__reduce_add_sync(0xffffffffu, k)) >= need) t = c;
+        __syncwarp();
+        best = 0;
+#pragma unroll 1
+        for (int k = 0; 32 * k < m; ++k) {       // (to places before their own: those of earlier rounds, and of this one, are read)
+            const bool mine = (keep >> k) & 1;
+            const double d = mine ? s.all[lane + 32 * k] : 0.0;
+            const int page = mine ? s.page[lane + 32 * k] : 0;
+            const uint32_t t = __ballot_sync(0xffffffffu, mine);
+            if (mine) {
+                const int at = best + __popc(t & ((1u << lane) - 1));
+                s.all[at] = d;
+                s.page[at] = page;
+            }
+            best += __popc(t);
+            __syncwarp();
         }
-        const float floor = t < 0x00800000u ? -INFINITY : key_value(t) - 2.f * delta;      // (maxima of nothing: every page)
-        const int m = pick_gather(s, row, begin, end, floor);
-        if (m <= kPickGather && pick_settle(s, w, m, need, delta)) return;
     }
-    pick_thorough(s, w, row, begin, end, need, delta);
 }
 
 // The first work_blocks blocks pick; the block after them, if there is one, writes the status.
-__global__ void __launch_bounds__(kPickThreads) block_pick_kernel(const SelectParams p, const int work_blocks) {
+__global__ void __launch_bounds__(kPickThreads, 4) block_pick_kernel(const SelectParams p, const int work_blocks) {
     extern __shared__ __align__(16) uint8_t pick_smem[];
     PickScratch* const scratch = reinterpret_cast<PickScratch*>(pick_smem);
     int32_t* const cu = reinterpret_cast<int32_t*>(pick_smem + kPickSmem);
@@ -620,7 +680,8 @@ __global__ void __launch_bounds__(kPickThreads) block_pick_kernel(const SelectPa
         return;
     }
     if (!scan_lengths<kPickThreads>(p.prefix_len, p.chunk_len, p.num_reqs, p.capacity, p.total_q, cu)) return;
-    const int G = p.num_q_heads / p.num_kv_heads;
+    const int G = p.num_q_heads / p.num_kv_heads, need = p.topk - p.num_first - p.num_last;
+    PickScratch& s = scratch[warp];
     const long long rows = static_cast<long long>(p.row1 - p.row0) * p.num_kv_heads, step = static_cast<long long>(work_blocks) * (kPickThreads / 32);
     for (long long i = static_cast<long long>(blockIdx.x) * (kPickThreads / 32) + warp; i < rows; i += step) {
         const int t = p.row0 + static_cast<int>(i / p.num_kv_heads), g = static_cast<int>(i % p.num_kv_heads);
@@ -631,26 +692,51 @@ __global__ void __launch_bounds__(kPickThreads) block_pick_kernel(const SelectPa
             for (int k = lane; k < p.topk; k += 32) out[k] = k <= own ? k : -1;
             continue;
         }
-        const int end = select_end(p, own), need = p.topk - p.num_first - p.num_last;      // (own + 1 > topk >= first + last: no overlap)
-        if (need > 0) {
-            float delta = 0.f;
-            bool odd = false;
-            const float* b = p.bounds + i * p.runs;
-            for (int k = p.num_first / p.run_pages + lane; k * p.run_pages < end; k += 32) {
-                const float x = b[k];
-                odd |= !(x < INFINITY);
-                delta = fmaxf(delta, x);
-            }
+        // (own + 1 > topk >= first + last: the two ends do not meet, and there are more candidates than needed)
+        const int end = select_end(p, own), run0 = p.num_first / p.run_pages, runs = (end + p.run_pages - 1) / p.run_pages;
+        for (int k = lane; k < p.topk; k += 32)
+            if (k < p.num_first || k >= p.num_first + need) out[k] = k < p.num_first ? k : own + 1 - (p.topk - k);
+        if (need == 0) continue;
+        float delta = 0.f;
+        bool odd = false;
+        for (int k = run0 + lane; k < runs; k += 32) {
+            const float x = p.bounds[i * p.runs + k];
+            odd |= !(x < INFINITY);
+            delta = fmaxf(delta, x);
+        }
 #pragma unroll
-            for (int o = 16; o > 0; o >>= 1) delta = fmaxf(delta, __shfl_xor_sync(0xffffffffu, delta, o));
-            if (__any_sync(0xffffffffu, odd)) delta = INFINITY;
-            const PickRow w{p.q + (static_cast<long long>(t) * p.num_q_heads + g * G) * 256, p.block_table + static_cast<long long>(r) * p.max_blocks_per_req,
-                            p.means + g * 256, static_cast<long long>(p.num_kv_heads) * 256, G, p.num_blocks};
-            pick(scratch[warp], w, p.scores + i * p.row_pages, p.num_first, end, need, delta);
+        for (int o = 16; o > 0; o >>= 1) delta = fmaxf(delta, __shfl_xor_sync(0xffffffffu, delta, o));
+        odd = __any_sync(0xffffffffu, odd);
+        if (!odd && delta == 0.f) {       // all scores are 0
+            for (int k = lane; k < need; k += 32) out[p.num_first + k] = p.num_first + k;
+            continue;
+        }
+        const PickRow w{p.q + (static_cast<long long>(t) * p.num_q_heads + g * G) * 256, p.block_table + static_cast<long long>(r) * p.max_blocks_per_req,
+                        p.means + g * 256, static_cast<long long>(p.num_kv_heads) * 256, G, p.num_blocks};
+        // the runs' candidates, one behind the other
+        int m = 0;
+        for (int k = 2 * run0; k < 2 * runs && !odd; ++k) {
+            const int c = p.counts[i * p.runs * 2 + k];
+            odd = c > p.cap || m + c > kPickGather || !(p.bounds[i * p.runs + (k >> 1)] > 0.f);      // (a run whose scores are all 0 lists none)
+            if (odd) break;
+            const SelectCandidate* const from = p.found + (i * p.runs * 2 + k) * p.cap;
+            for (int j = lane; j < c; j += 32) {
+                const SelectCandidate x = from[j];
+                s.score[m + j] = x.score;
+                s.page[m + j] = x.page;
+            }
+            m += c;
         }
         __syncwarp();
-        for (int k = lane; k < p.topk; k += 32)
-            out[k] = k < p.num_first ? k : k < p.num_first + need ? scratch[warp].page[k - p.num_first] : own + 1 - (p.topk - k);
+        if (odd || !pick_settle(s, w, m, need, delta)) pick_thorough(s, w, p.num_first, end, need);
+        __syncwarp();
+        // ascending
+        for (int k = lane; k < need; k += 32) {
+            const int page = s.page[k];
+            int before = 0;
+            for (int j = 0; j < need; ++j) before += s.page[j] < page;
+            out[p.num_first + before] = page;
+        }
         __syncwarp();
     }
 }

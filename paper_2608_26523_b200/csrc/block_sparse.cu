@@ -80,11 +80,11 @@ vpp_status check_paged(const int32_t* block_table, int block_size, int max_block
 
 // ---- page selection: slabs of tokens, and where their scores are ----
 struct SelectPlan {
-    int row_pages;        // floats of a row of scores
-    int slab;             // tokens of a slab
-    int run_pages, runs;  // pages of an item, items along a row
-    int items;            // most items of a slab
-    size_t scores, bounds, bad, total;
+    int slab;                   // tokens of a slab
+    int run_pages, runs;        // pages of an item, items along a row
+    int group_pages, cap;
+    int items;                  // most items of a slab
+    size_t found, counts, bounds, maxima, bad, total;
 };
 
 vpp_status select_plan(const vpp_block_select_args* a, SelectPlan* s) {
@@ -99,30 +99,43 @@ vpp_status select_plan(const vpp_block_select_args* a, SelectPlan* s) {
     if (a->topk < 1 || a->topk > vpp::kSelectMaxTopk) return fail(VPP_ERR_UNSUPPORTED, "topk must be in 1..%d", vpp::kSelectMaxTopk);
     if (a->num_first < 0 || a->num_last < 1 || a->num_first > a->topk || a->num_last > a->topk - a->num_first)
         return fail(VPP_ERR_INVALID_ARG, "need num_first >= 0, num_last >= 1 and num_first + num_last <= topk");
-    const long long T = a->total_q > 0 ? a->total_q : 1, H = a->num_kv_heads;
-    const long long pages = a->max_seq_len / a->block_size + 1;
-    s->row_pages = static_cast<int>((pages + vpp::kSelectTile - 1) / vpp::kSelectTile * vpp::kSelectTile);
-    long long slab = vpp::kSelectSlabBytes / (4ll * s->row_pages * H);
-    slab = slab / vpp::kSelectTile * vpp::kSelectTile;         // (whole tiles of a long chunk)
-    if (slab < vpp::kSelectTile) slab = vpp::kSelectTile;
+    const long long T = a->total_q > 0 ? a->total_q : 1, H = a->num_kv_heads, N = vpp::kSelectTile;
+    const long long steps = (a->max_seq_len / a->block_size + N) / N;       // of 128 pages along a row
+    const int need = a->topk - a->num_first - a->num_last;
+    // A border that is the need-th largest of the maxima of groups lets through about need (1 + need * group / (2 * pages)) pages.  Rows of few pages
+    // list them all, others have pages enough for twice as many groups as are needed.
+    s->group_pages = need <= 32 ? 8 : need <= 64 ? 4 : need <= 128 ? 2 : 1;
+    s->cap = need <= 128 ? 128 : 256;
+    auto tiles_of = [&](long long rows) {
+        const long long tiles = (rows + N - 1) / N + a->num_reqs;
+        return tiles < rows ? tiles : rows;           // (every tile has a token)
+    };
+    // runs of pages: one where the tiles fill the SMs twice, else as many as do (each lists its own best)
+    long long runs = 2ll * sm_count_or_default() / (tiles_of(T) * H);
+    if (runs > 4) runs = 4;
+    if (runs > steps / 2) runs = steps / 2;
+    const long long least = (steps * N + vpp::kSelectMaxRun - 1) / vpp::kSelectMaxRun;
+    if (runs < least) runs = least;
+    if (runs < 1) runs = 1;
+    s->run_pages = static_cast<int>((steps + runs - 1) / runs * N);
+    s->runs = static_cast<int>((steps * N + s->run_pages - 1) / s->run_pages);
+    const long long list = s->runs * (2ll * s->cap * static_cast<long long>(sizeof(vpp::SelectCandidate)) + 12);     // bytes of a row
+    const long long item = N * (s->run_pages / s->group_pages) * 4;                                                  // of an item
+    long long slab = vpp::kSelectSlabBytes / (H * (list + item * s->runs / N));
+    slab = slab / N * N;                              // (whole tiles of a long chunk)
+    if (slab < N) slab = N;
     if (slab > T) slab = T;
     s->slab = static_cast<int>(slab);
-    // runs of pages: one where the tiles fill the SMs, else as many as give each about one item
-    const long long tiles_ub = (slab + vpp::kSelectTile - 1) / vpp::kSelectTile + a->num_reqs;
-    const long long tiles = tiles_ub < slab ? tiles_ub : slab;           // (every tile has a token)
-    const long long steps = s->row_pages / vpp::kSelectTile;
-    long long runs = (2ll * sm_count_or_default()) / (tiles * H);
-    if (runs < 1) runs = 1;
-    if (runs > steps) runs = steps;
-    s->run_pages = static_cast<int>((steps + runs - 1) / runs) * vpp::kSelectTile;
-    s->runs = (s->row_pages + s->run_pages - 1) / s->run_pages;
-    const long long items = tiles * H * s->runs;
+    const long long items = tiles_of(slab) * H * s->runs;
     if (items > INT32_MAX) return fail(VPP_ERR_UNSUPPORTED, "too many requests times heads");
     s->items = static_cast<int>(items);
-    s->scores = 0;
-    s->bounds = align_up(s->scores + static_cast<size_t>(slab) * H * s->row_pages * 4, 256);
-    s->bad = align_up(s->bounds + static_cast<size_t>(slab) * H * s->runs * 4, 256);
-    s->total = align_up(s->bad + static_cast<size_t>(s->items) * 4, 256);
+    const size_t rows = static_cast<size_t>(slab) * H * s->runs;
+    s->found = 0;
+    s->counts = align_up(rows * 2 * s->cap * sizeof(vpp::SelectCandidate), 256);
+    s->bounds = align_up(s->counts + rows * 2 * sizeof(int32_t), 256);
+    s->maxima = align_up(s->bounds + rows * sizeof(float), 256);
+    s->bad = align_up(s->maxima + static_cast<size_t>(items) * item, 256);
+    s->total = align_up(s->bad + static_cast<size_t>(items) * sizeof(int32_t), 256);
     return VPP_OK;
 }
 
@@ -320,8 +333,10 @@ vpp_status vpp_block_means(const vpp_block_means_args* a, vpp_stream_t stream_) 
     const long long cap = 16ll * sm_count_or_default();
     if (blocks > cap) blocks = cap;
     const int work_blocks = static_cast<int>(blocks);
-    const cudaError_t ce = launch(vpp::block_means_kernel, static_cast<unsigned>(work_blocks + (a->status ? 1 : 0)), vpp::kMeansThreads,
-                                  sizeof(int32_t) * (static_cast<size_t>(a->num_reqs) + 1), stream, p, work_blocks);
+    cudaError_t ce = cudaSuccess;
+    if (a->num_reqs > 4096) ce = cudaFuncSetAttribute(vpp::block_means_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * 4 * (vpp::kLengthsMaxReqs + 1));
+    if (ce == cudaSuccess) ce = launch(vpp::block_means_kernel, static_cast<unsigned>(work_blocks + (a->status ? 1 : 0)), vpp::kMeansThreads,
+                                  2 * sizeof(int32_t) * (static_cast<size_t>(a->num_reqs) + 1), stream, p, work_blocks);
     if (ce != cudaSuccess) return fail(VPP_ERR_CUDA, "page means launch: %s", cudaGetErrorString(ce));
     return VPP_OK;
 }
@@ -357,7 +372,7 @@ vpp_status vpp_block_select(const vpp_block_select_args* a, vpp_stream_t stream_
     p.max_blocks_per_req = a->max_blocks_per_req;
     p.block_shift = ilog2(a->block_size);
     p.num_blocks = a->num_blocks;
-    // rows of scores are as long as max_seq_len has pages, and the table as wide as max_blocks_per_req
+    // the runs go as far as max_seq_len has pages, and the table as max_blocks_per_req
     p.capacity = paged_capacity(a->max_blocks_per_req, a->block_size);
     if (p.capacity > a->max_seq_len) p.capacity = a->max_seq_len;
     p.total_q = a->total_q;
@@ -368,22 +383,25 @@ vpp_status vpp_block_select(const vpp_block_select_args* a, vpp_stream_t stream_
     p.num_last = a->num_last;
     p.run_pages = s.run_pages;
     p.runs = s.runs;
-    p.row_pages = s.row_pages;
-    p.scores = reinterpret_cast<float*>(ws + s.scores);
+    p.group_pages = s.group_pages;
+    p.cap = s.cap;
+    p.found = reinterpret_cast<vpp::SelectCandidate*>(ws + s.found);
+    p.counts = reinterpret_cast<int32_t*>(ws + s.counts);
     p.bounds = reinterpret_cast<float*>(ws + s.bounds);
+    p.maxima = reinterpret_cast<float*>(ws + s.maxima);
     p.bad = reinterpret_cast<int32_t*>(ws + s.bad);
     p.items = s.items;
     p.indices = a->indices;
     p.status = a->status;
     const size_t lens = sizeof(int32_t) * (static_cast<size_t>(a->num_reqs) + 1);
     const size_t smem_scores = vpp::kSelectSmem + 2 * lens, smem_pick = vpp::kPickSmem + lens;
-    cudaError_t ce = cudaFuncSetAttribute(vpp::block_scores_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem_scores));
+    cudaError_t ce = cudaFuncSetAttribute(vpp::block_filter_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem_scores));
     if (ce == cudaSuccess) ce = cudaFuncSetAttribute(vpp::block_pick_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem_pick));
     if (ce != cudaSuccess) return fail(VPP_ERR_CUDA, "page selection attributes: %s", cudaGetErrorString(ce));
     for (int64_t row0 = 0; row0 < a->total_q; row0 += s.slab) {
         p.row0 = static_cast<int32_t>(row0);
         p.row1 = static_cast<int32_t>(row0 + s.slab < a->total_q ? row0 + s.slab : a->total_q);
-        ce = launch(vpp::block_scores_kernel, static_cast<unsigned>(s.items), vpp::kSelectThreads, smem_scores, stream, p);
+        ce = launch(vpp::block_filter_kernel, static_cast<unsigned>(s.items), vpp::kSelectThreads, smem_scores, stream, p);
         if (ce != cudaSuccess) return fail(VPP_ERR_CUDA, "page scores launch: %s", cudaGetErrorString(ce));
         const long long rows = static_cast<long long>(p.row1 - p.row0) * a->num_kv_heads, warps = vpp::kPickThreads / 32;
         long long blocks = (rows + warps - 1) / warps;

@@ -6,49 +6,51 @@ namespace vpp {
 
 constexpr int kLengthsMaxReqs = 8192;   // the scan of chunk_len lives in shared memory (32 KB + 4)
 
+// Exclusive sums of count(i), i = 0 .. n - 1, into out[0 .. n] (shared memory), by a whole block of kThreads; the sums stop at `most`.  Ends
+// with a barrier.  Returns whether any thread was `bad`.
+template <int kThreads, typename Count>
+__device__ __forceinline__ bool block_scan(int n, uint32_t most, int32_t* out, bool bad, Count count) {
+    __shared__ uint32_t s_warp[2][kThreads / 32];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    uint32_t carry = 0;
+    for (int base = 0, round = 0; base < n; base += kThreads, round ^= 1) {
+        const int i = base + tid;
+        const uint32_t c = i < n ? static_cast<uint32_t>(count(i, bad)) : 0u;
+        uint32_t x = c;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t y = __shfl_up_sync(0xffffffffu, x, o);
+            if (lane >= o) x = min(x + y, most);
+        }
+        if (lane == 31) s_warp[round][warp] = x;
+        __syncthreads();
+        uint32_t before = carry;
+#pragma unroll
+        for (int w = 0; w < kThreads / 32; ++w) {
+            if (w == warp) before = carry;
+            carry = min(carry + s_warp[round][w], most);
+        }
+        uint32_t left = __shfl_up_sync(0xffffffffu, x, 1);
+        if (lane == 0) left = 0;
+        if (i < n) out[i] = static_cast<int32_t>(min(before + left, most));
+    }
+    if (tid == 0) out[n] = static_cast<int32_t>(carry);
+    return __syncthreads_or(bad);
+}
+
 // Exclusive scan of chunk_len into cu[0 .. num_reqs] (shared memory), by a whole block of kThreads; true if the lengths describe
-// the launch: none negative, no request past `capacity` positions, their sum total_q.  (The sums are formed in 64 bits: lengths that
-// wrap around to total_q must not pass.)
+// the launch: none negative, no request past `capacity` positions, their sum total_q.  (Sums stop at total_q + 1: lengths that would wrap around to
+// total_q do not pass.)
 template <int kThreads>
 __device__ __forceinline__ bool scan_lengths(const int32_t* prefix_len, const int32_t* chunk_len, int num_reqs, long long capacity,
                                              int total_q, int32_t* cu) {
-    __shared__ int s_bad;
-    const int tid = threadIdx.x, lane = tid & 31;
-    if (tid == 0) s_bad = 0;
-    __syncthreads();
-    bool bad = false;
-    for (int r = tid; r < num_reqs; r += kThreads) {   // (all loads at once, then the scan from shared memory)
-        int c = chunk_len[r];
-        const int pre = prefix_len[r];
-        if (c < 0 || c > total_q || pre < 0 || static_cast<long long>(pre) + c > capacity) {
-            bad = true;
-            c = 0;
-        }
-        cu[r] = c;
-    }
-    if (bad) s_bad = 1;
-    __syncthreads();
-    if (tid < 32) {
-        long long carry = 0;
-        for (int base = 0; base < num_reqs; base += 32) {
-            const int r = base + lane;
-            const int c = r < num_reqs ? cu[r] : 0;
-            long long x = c;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const long long y = __shfl_up_sync(0xffffffffu, x, o);
-                if (lane >= o) x += y;
-            }
-            if (r < num_reqs) cu[r] = static_cast<int32_t>(carry + x - c);
-            carry += __shfl_sync(0xffffffffu, x, 31);
-        }
-        if (lane == 0) {
-            cu[num_reqs] = static_cast<int32_t>(carry);
-            if (carry != total_q) s_bad = 1;
-        }
-    }
-    __syncthreads();
-    return !s_bad;
+    const bool bad = block_scan<kThreads>(num_reqs, static_cast<uint32_t>(total_q) + 1u, cu, false, [&](int r, bool& is_bad) {
+        const int c = chunk_len[r], pre = prefix_len[r];
+        if (c >= 0 && c <= total_q && pre >= 0 && static_cast<long long>(pre) + c <= capacity) return c;
+        is_bad = true;
+        return 0;
+    });
+    return !bad && cu[num_reqs] == total_q;
 }
 
 // Request of row g (0 <= g < total_q): the last r with cu[r] <= g.
