@@ -5,6 +5,7 @@ streams.  There is no CPU fallback: if the shared library is missing or cannot b
 """
 import ctypes
 import os
+import struct
 
 import torch
 
@@ -130,6 +131,13 @@ class BlockSelectArgs(ctypes.Structure):
     ]
 
 
+# The same structs as format strings: the calls of a decode step take as long on the host as on the GPU, and packing a struct's bytes takes half as long as
+# filling a ctypes.Structure (vpp_kv_append_rope 15 -> 7 us a call, vpp_rope 8 -> 4).
+_PACK_ROPE = struct.Struct("PPqqqqPPiiiiPiiifP")
+_PACK_APPEND_ROPE = struct.Struct("PPPPqqqqqqPPPiiiiiiiiiPqqqqPPqqqqiPiiif")
+_PACK_MEANS = struct.Struct("PqqqPPPPiiiiiiiP")
+_PACK_SELECT = struct.Struct("PPPPPiiiiiiiiiiiiPPNP")
+
 _lib = None
 
 
@@ -179,15 +187,15 @@ def load_library():
         lib.vpp_chunk_attn_host_fwd.argtypes = [ctypes.POINTER(HostChunkAttnArgs), ctypes.c_void_p]
         lib.vpp_host_last_error.restype = ctypes.c_char_p
         lib.vpp_rope.restype = ctypes.c_int
-        lib.vpp_rope.argtypes = [ctypes.POINTER(RopeArgs), ctypes.c_void_p]
+        lib.vpp_rope.argtypes = [ctypes.c_char_p, ctypes.c_void_p]            # (a struct's bytes: see _PACK_ROPE)
         lib.vpp_kv_append_rope.restype = ctypes.c_int
-        lib.vpp_kv_append_rope.argtypes = [ctypes.POINTER(KvAppendRopeArgs), ctypes.c_void_p]
+        lib.vpp_kv_append_rope.argtypes = [ctypes.c_char_p, ctypes.c_void_p]
         lib.vpp_block_means.restype = ctypes.c_int
-        lib.vpp_block_means.argtypes = [ctypes.POINTER(BlockMeansArgs), ctypes.c_void_p]
+        lib.vpp_block_means.argtypes = [ctypes.c_char_p, ctypes.c_void_p]
         lib.vpp_block_select_workspace_size.restype = ctypes.c_size_t
         lib.vpp_block_select_workspace_size.argtypes = [ctypes.POINTER(BlockSelectArgs)]
         lib.vpp_block_select.restype = ctypes.c_int
-        lib.vpp_block_select.argtypes = [ctypes.POINTER(BlockSelectArgs), ctypes.c_void_p]
+        lib.vpp_block_select.argtypes = [ctypes.c_char_p, ctypes.c_void_p]
         lib.vpp_block_attn_workspace_size.restype = ctypes.c_size_t
         lib.vpp_block_attn_workspace_size.argtypes = [ctypes.POINTER(ChunkAttnArgs), ctypes.c_int32]
         lib.vpp_block_attn_fwd.restype = ctypes.c_int
@@ -342,15 +350,15 @@ def vpp_rope(x, out, prefix_len, chunk_len, inv_freq, layout="half", rot_offset=
 
     x, out [T, H, D] bf16, any strides with a contiguous last dim (out may be x); inv_freq fp32 [rot_dim / 2]; layout "half"
     (feature j with j + rot_dim / 2) or "interleaved" (2 j with 2 j + 1)."""
-    assert x.shape == out.shape and x.dtype == out.dtype == torch.bfloat16 and x.stride(2) == 1 and out.stride(2) == 1
-    assert inv_freq.dtype == torch.float32 and inv_freq.is_contiguous()
-    a = RopeArgs(x.data_ptr(), out.data_ptr(), x.stride(0), x.stride(1), out.stride(0), out.stride(1), prefix_len.data_ptr(),
-                 chunk_len.data_ptr(), prefix_len.numel(), x.shape[0], x.shape[1], x.shape[2],
-                 RopeSpec(inv_freq.data_ptr(), 2 * inv_freq.numel(), int(rot_offset), ROPE_LAYOUTS[layout], float(amplitude)),
-                 None if status is None else status.data_ptr())
-    if stream is None:
-        stream = _current_stream()
-    _check(load_library().vpp_rope(ctypes.byref(a), stream))
+    shape, xs, os_ = x.shape, x.stride(), out.stride()
+    assert shape == out.shape and x.dtype is out.dtype is torch.bfloat16 and xs[2] == 1 == os_[2]
+    assert inv_freq.dtype is torch.float32 and inv_freq.is_contiguous()
+    a = _PACK_ROPE.pack(x.data_ptr(), out.data_ptr(), xs[0], xs[1], os_[0], os_[1], prefix_len.data_ptr(), chunk_len.data_ptr(),
+                        prefix_len.numel(), shape[0], shape[1], shape[2], inv_freq.data_ptr(), 2 * inv_freq.numel(), rot_offset,
+                        ROPE_LAYOUTS[layout], amplitude, 0 if status is None else status.data_ptr())
+    rc = load_library().vpp_rope(a, _current_stream() if stream is None else stream)
+    if rc:
+        _check(rc)
 
 
 def vpp_kv_append_rope(k_new, v_new, k_cache, v_cache, block_table, prefix_len, chunk_len, block_size, max_seq_len, inv_freq, q=None,
@@ -358,41 +366,46 @@ def vpp_kv_append_rope(k_new, v_new, k_cache, v_cache, block_table, prefix_len, 
     """vpp_kv_append with the keys rotated to their positions on the way, and q [T, Hq, Dqk] rotated into q_out (both or neither).
 
     k_new, v_new, q, q_out: any strides with a contiguous last dim, as slices of a fused projection have them."""
-    ks, vs = k_cache.stride(), v_cache.stride() if v_cache is not None else (0, 0, 0, 1)
-    assert ks[3] == 1 and vs[3] == 1 and k_new.stride(2) == 1 and (v_new is None or v_new.stride(2) == 1)
-    assert all(t is None or t.dtype == torch.bfloat16 for t in (k_new, v_new, q, q_out, k_cache, v_cache))
-    assert inv_freq.dtype == torch.float32 and inv_freq.is_contiguous()
-    assert (q is None) == (q_out is None)
-    assert q is None or (q.shape == q_out.shape and q.stride(2) == 1 and q_out.stride(2) == 1 and q.shape[0] == k_new.shape[0] and q.shape[2] == k_new.shape[2])
-    head_dim_v = v_new.shape[2] if v_new is not None else (v_cache.shape[3] if v_cache is not None else k_new.shape[2])
-    append = KvAppendArgs(
-        k_new.data_ptr(), None if v_new is None else v_new.data_ptr(), k_cache.data_ptr(),
-        None if v_cache is None else v_cache.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2],
-        None if block_table is None else block_table.data_ptr(), prefix_len.data_ptr(), chunk_len.data_ptr(),
-        prefix_len.numel(), 0 if block_table is None else block_table.shape[1], int(block_size), k_cache.shape[0],
-        k_new.shape[0], int(max_seq_len), k_new.shape[1], k_new.shape[2], head_dim_v, None if status is None else status.data_ptr())
-    n_s, v_s = k_new.stride(), v_new.stride() if v_new is not None else (0, 0)
-    q_s, o_s = (q.stride(), q_out.stride()) if q is not None else ((0, 0), (0, 0))
-    a = KvAppendRopeArgs(append, n_s[0], n_s[1], v_s[0], v_s[1], None if q is None else q.data_ptr(),
-                         None if q is None else q_out.data_ptr(), q_s[0], q_s[1], o_s[0], o_s[1], 0 if q is None else q.shape[1],
-                         RopeSpec(inv_freq.data_ptr(), 2 * inv_freq.numel(), int(rot_offset), ROPE_LAYOUTS[layout], float(amplitude)))
-    if stream is None:
-        stream = _current_stream()
-    _check(load_library().vpp_kv_append_rope(ctypes.byref(a), stream))
+    bf16 = torch.bfloat16
+    shape, ns, ks = k_new.shape, k_new.stride(), k_cache.stride()
+    assert k_new.dtype is k_cache.dtype is bf16 and ns[2] == 1 == ks[3]
+    assert inv_freq.dtype is torch.float32 and inv_freq.is_contiguous()
+    if v_new is not None:
+        v_ptr, vn, vs, dim_v = v_new.data_ptr(), v_new.stride(), v_cache.stride(), v_new.shape[2]
+        assert v_new.dtype is v_cache.dtype is bf16 and vn[2] == 1 == vs[3] and v_new.shape[:2] == shape[:2]
+    else:
+        v_ptr, vn, vs, dim_v = 0, (0, 0), (0, 0, 0), shape[2] if v_cache is None else v_cache.shape[3]
+    if q is not None:
+        q_shape, qs, os_ = q.shape, q.stride(), q_out.stride()
+        assert q_shape == q_out.shape and q.dtype is q_out.dtype is bf16 and qs[2] == 1 == os_[2]
+        assert q_shape[0] == shape[0] and q_shape[2] == shape[2]
+        q_part = (q.data_ptr(), q_out.data_ptr(), qs[0], qs[1], os_[0], os_[1], q_shape[1])
+    else:
+        assert q_out is None
+        q_part = (0, 0, 0, 0, 0, 0, 0)
+    a = _PACK_APPEND_ROPE.pack(
+        k_new.data_ptr(), v_ptr, k_cache.data_ptr(), 0 if v_cache is None else v_cache.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2],
+        0 if block_table is None else block_table.data_ptr(), prefix_len.data_ptr(), chunk_len.data_ptr(), prefix_len.numel(),
+        0 if block_table is None else block_table.shape[1], block_size, k_cache.shape[0], shape[0], max_seq_len, shape[1], shape[2], dim_v,
+        0 if status is None else status.data_ptr(), ns[0], ns[1], vn[0], vn[1], *q_part,
+        inv_freq.data_ptr(), 2 * inv_freq.numel(), rot_offset, ROPE_LAYOUTS[layout], amplitude)
+    rc = load_library().vpp_kv_append_rope(a, _current_stream() if stream is None else stream)
+    if rc:
+        _check(rc)
 
 
 def vpp_block_means(k_cache, k_means, block_table, prefix_len, chunk_len, block_size, total_q, status=None, stream=None):
     """k_means[page] <- mean key of every page that the chunk completes.  k_cache [num_blocks, block_size, Hkv, 128], any strides with a
     contiguous last dim; k_means [num_blocks, Hkv, 128] bf16, dense."""
-    ks = k_cache.stride()
-    assert ks[3] == 1 and k_means.is_contiguous() and k_cache.dtype == k_means.dtype == torch.bfloat16
-    assert k_means.shape == (k_cache.shape[0], k_cache.shape[2], k_cache.shape[3])
-    a = BlockMeansArgs(k_cache.data_ptr(), ks[0], ks[1], ks[2], k_means.data_ptr(), _ptr(block_table), prefix_len.data_ptr(), chunk_len.data_ptr(),
-                       prefix_len.numel(), 0 if block_table is None else block_table.shape[1], int(block_size), k_cache.shape[0], int(total_q),
-                       k_cache.shape[2], k_cache.shape[3], None if status is None else status.data_ptr())
-    if stream is None:
-        stream = _current_stream()
-    _check(load_library().vpp_block_means(ctypes.byref(a), stream))
+    ks, shape = k_cache.stride(), k_cache.shape
+    assert ks[3] == 1 and k_means.is_contiguous() and k_cache.dtype is k_means.dtype is torch.bfloat16
+    assert k_means.shape == (shape[0], shape[2], shape[3])
+    a = _PACK_MEANS.pack(k_cache.data_ptr(), ks[0], ks[1], ks[2], k_means.data_ptr(), 0 if block_table is None else block_table.data_ptr(),
+                         prefix_len.data_ptr(), chunk_len.data_ptr(), prefix_len.numel(), 0 if block_table is None else block_table.shape[1],
+                         block_size, shape[0], total_q, shape[2], shape[3], 0 if status is None else status.data_ptr())
+    rc = load_library().vpp_block_means(a, _current_stream() if stream is None else stream)
+    if rc:
+        _check(rc)
 
 
 def vpp_block_select_workspace_size(total_q, num_reqs, num_q_heads, num_kv_heads, block_size, max_seq_len, topk=None):
@@ -408,16 +421,17 @@ def vpp_block_select(q, k_means, block_table, prefix_len, chunk_len, block_size,
                      status=None, stream=None):
     """indices [T, Hkv, topk] int32 <- the pages that each token's queries score highest (see include/vpp.h).  q [T, Hq, 128] bf16 dense,
     k_means [num_blocks, Hkv, 128]; workspace of vpp_block_select_workspace_size(...) bytes."""
-    assert q.is_contiguous() and k_means.is_contiguous() and indices.is_contiguous() and indices.dtype == torch.int32
-    assert indices.shape[:2] == (q.shape[0], k_means.shape[1]) and q.dtype == k_means.dtype == torch.bfloat16 and q.shape[2] == k_means.shape[2]
-    a = BlockSelectArgs(q.data_ptr(), k_means.data_ptr(), _ptr(block_table), prefix_len.data_ptr(), chunk_len.data_ptr(),
-                        prefix_len.numel(), 0 if block_table is None else block_table.shape[1], int(block_size), k_means.shape[0], q.shape[0],
-                        int(max_seq_len), q.shape[1], k_means.shape[1], q.shape[2], indices.shape[2], int(num_first), int(num_last),
-                        indices.data_ptr(), _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
-                        None if status is None else status.data_ptr())
-    if stream is None:
-        stream = _current_stream()
-    _check(load_library().vpp_block_select(ctypes.byref(a), stream))
+    q_shape, i_shape = q.shape, indices.shape
+    assert q.is_contiguous() and k_means.is_contiguous() and indices.is_contiguous() and indices.dtype is torch.int32
+    assert i_shape[0] == q_shape[0] and i_shape[1] == k_means.shape[1] and q.dtype is k_means.dtype is torch.bfloat16 and q_shape[2] == k_means.shape[2]
+    a = _PACK_SELECT.pack(q.data_ptr(), k_means.data_ptr(), 0 if block_table is None else block_table.data_ptr(), prefix_len.data_ptr(),
+                          chunk_len.data_ptr(), prefix_len.numel(), 0 if block_table is None else block_table.shape[1], block_size, k_means.shape[0], q_shape[0],
+                          max_seq_len, q_shape[1], k_means.shape[1], q_shape[2], i_shape[2], num_first, num_last, indices.data_ptr(),
+                          0 if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel() * workspace.element_size(),
+                          0 if status is None else status.data_ptr())
+    rc = load_library().vpp_block_select(a, _current_stream() if stream is None else stream)
+    if rc:
+        _check(rc)
 
 
 def vpp_block_attn_workspace_size(args, topk):
@@ -426,10 +440,9 @@ def vpp_block_attn_workspace_size(args, topk):
 
 def vpp_block_attn_fwd(args, indices, stream=None):
     """Attention of the launch described by `args` (make_args) over the pages listed in indices [T, Hkv, topk] int32."""
-    assert indices.dtype == torch.int32 and indices.is_contiguous() and indices.shape[:2] == (args.total_q, args.num_kv_heads)
-    if stream is None:
-        stream = _current_stream()
-    _check(load_library().vpp_block_attn_fwd(ctypes.byref(args), indices.data_ptr(), indices.shape[2], stream))
+    shape = indices.shape
+    assert indices.dtype is torch.int32 and indices.is_contiguous() and shape[0] == args.total_q and shape[1] == args.num_kv_heads
+    _check(load_library().vpp_block_attn_fwd(ctypes.byref(args), indices.data_ptr(), shape[2], _current_stream() if stream is None else stream))
 
 
 def vpp_sparse_attn_workspace_size(total_q):

@@ -57,12 +57,12 @@ struct SelectParams {
     int topk, num_first, num_last;
     int row0, row1;               // this slab's tokens
     int run_pages, runs;          // pages of an item (a multiple of 128), items along a row
-    int group_pages;              // pages of a group of which the maximum is kept (8, 4, 2, 1)
+    int group_pages;              // pages of a group of which the maximum is kept (4, 2, 1; 0: 64 groups of every 64th page or so, in registers)
     int cap;                      // candidates of half an item's pages, at most
     SelectCandidate* found;       // [row1 - row0, Hkv, runs, 2, cap]
     int32_t* counts;              // [row1 - row0, Hkv, runs, 2] (past cap: more than fit)
     float* bounds;                // [row1 - row0, Hkv, runs]: error bound of the row's scores of a run
-    float* maxima;                // [items, 128, run_pages / group_pages]
+    float* maxima;                // [items, 128, run_pages / group_pages] (group_pages > 0)
     int32_t* bad;                 // one word an item of the slab
     int items;
     int32_t* indices;             // [total_q, Hkv, topk]
@@ -373,15 +373,19 @@ __global__ void __launch_bounds__(kSelectThreads, 2) block_filter_kernel(const S
     constexpr uint32_t kIdesc = idesc_bf16(kSelectTile, kSelectTile, false, false), kHi = desc_hi_sw128(1024);
     const int my_row = (warp & 3) * 32 + lane, half = warp >> 2;
     const int stop = my_row < n ? end_of(my_row) : 0;
-    const int gp = p.group_pages, row_groups = p.run_pages / gp;
+    const int gp = p.group_pages, row_groups = gp > 0 ? p.run_pages / gp : 0;
     float* const my_maxima = p.maxima + (static_cast<long long>(item) * kSelectTile + my_row) * row_groups;
     // no more candidates than fit: no border is needed
     const bool filter = page1 - begin > p.cap;
     uint32_t phase = 0;
     bool alive = true;
-    float floor = -INFINITY;
-    int m = 0;
+    float floor = -3.4e38f;      // (below every score that counts and above the -inf of pages that are no candidates)
     SelectCandidate* const found = p.found + (list_of(my_row) * 2 + half) * p.cap;
+    SelectCandidate* to_next = found;
+    int m = 0;                   // those that found no room
+    float mx[32];                // gp == 0: of the pages that are column i of a piece
+#pragma unroll
+    for (int i = 0; i < 32; ++i) mx[i] = -INFINITY;
     for (int pass = filter ? 0 : 1; pass < 2 && alive; ++pass) {
         for (int j0 = page0; j0 < page1; j0 += kSelectTile) {
             const bool more = j0 + kSelectTile < page1;
@@ -389,7 +393,7 @@ __global__ void __launch_bounds__(kSelectThreads, 2) block_filter_kernel(const S
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int t = (tid >> 4) + 16 * i;
-                top = abs_max(top, x[i]);
+                if (pass == 0 || !filter) top = abs_max(top, x[i]);
                 *reinterpret_cast<uint4*>(sB + (v >> 3) * (kSelectTile * 128) + t * 128 + (((v & 7) ^ (t & 7)) << 4)) = x[i];
             }
             fence_proxy_async_smem();
@@ -422,15 +426,15 @@ __global__ void __launch_bounds__(kSelectThreads, 2) block_filter_kernel(const S
                         if (j + i < begin || j + i >= stop) s[i] = 0xff800000u;   // -inf
                 }
                 if (pass == 0) {
-                    if (my_row < n) {
+                    if (gp == 0) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) mx[i] = fmaxf(mx[i], __uint_as_float(s[i]));
+                    } else if (my_row < n) {
                         float4* const to = reinterpret_cast<float4*>(my_maxima + (j - page0) / gp);
                         auto at = [&](int i) { return __uint_as_float(s[i]); };
                         auto two = [&](int i) { return fmaxf(at(2 * i), at(2 * i + 1)); };
                         auto four = [&](int i) { return fmax3(at(4 * i), at(4 * i + 1), fmaxf(at(4 * i + 2), at(4 * i + 3))); };
-                        auto eight = [&](int i) { return fmaxf(four(2 * i), four(2 * i + 1)); };
-                        if (gp == 8) {
-                            to[0] = make_float4(eight(0), eight(1), eight(2), eight(3));
-                        } else if (gp == 4) {
+                        if (gp == 4) {
 #pragma unroll
                             for (int i = 0; i < 2; ++i) to[i] = make_float4(four(4 * i), four(4 * i + 1), four(4 * i + 2), four(4 * i + 3));
                         } else if (gp == 2) {
@@ -441,15 +445,19 @@ __global__ void __launch_bounds__(kSelectThreads, 2) block_filter_kernel(const S
                             for (int i = 0; i < 8; ++i) to[i] = make_float4(at(4 * i), at(4 * i + 1), at(4 * i + 2), at(4 * i + 3));
                         }
                     }
-                } else {
-                    // (a page that is not a candidate is -inf: with a border of -inf it must be told by its number)
-                    const int last = stop - j, lead = begin - j;
+                } else if (to_next - found <= p.cap - 32) {      // (room for them all: no check at each)
 #pragma unroll
                     for (int i = 0; i < 32; ++i) {
                         const float y = __uint_as_float(s[i]);
-                        if (y >= floor && i < last && i >= lead) {
-                            if (m < p.cap) found[m] = SelectCandidate{y, j + i};
-                            ++m;
+                        if (y >= floor) *to_next++ = SelectCandidate{y, j + i};
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) {
+                        const float y = __uint_as_float(s[i]);
+                        if (y >= floor) {
+                            if (to_next - found < p.cap) *to_next++ = SelectCandidate{y, j + i};
+                            else ++m;
                         }
                     }
                 }
@@ -462,19 +470,51 @@ __global__ void __launch_bounds__(kSelectThreads, 2) block_filter_kernel(const S
         const uint32_t warp_top = __reduce_max_sync(0xffffffffu, top);
         if (lane == 0) atomicMax(s_max, warp_top);
         __syncthreads();
-        const int lead_group = (begin - page0) / gp;
-        for (int t = warp; t < n; t += kSelectThreads / 32) {
-            const int stop_t = end_of(t);
+        if (gp == 0) {
+            // a thread a token (each twice): its 64 maxima, half of them from the other half's thread through the operand's place
+            float* const other = reinterpret_cast<float*>(sB) + my_row;       // [32][128], twice: 32 KB
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+                if (half == 1) other[i * kSelectTile] = mx[i];
+            __syncthreads();
             float f = INFINITY;          // (lists without choice, or bounds that say nothing: no candidates)
-            const float bound = select_bound(s_a[t], *s_max);
-            if (stop_t > begin && bound > 0.f && bound < INFINITY) {
-                f = -INFINITY;
-                if (stop_t - begin > p.cap) {
-                    const float* const mx = p.maxima + (static_cast<long long>(item) * kSelectTile + t) * row_groups + lead_group;
-                    f = border_of((stop_t - page0 + gp - 1) / gp - lead_group, need, [&](int i) { return mx[i]; }) - 2.f * bound;
+            if (half == 0) {
+                const float bound = my_row < n ? select_bound(s_a[my_row], *s_max) : 0.f;
+                if (stop > begin && bound > 0.f && bound < INFINITY) {
+                    f = -3.4e38f;
+                    if (stop - begin > p.cap) {
+                        float mo[32];
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) mo[i] = other[i * kSelectTile];
+                        uint32_t t = 0;      // the need-th largest of them, 16 bits of it
+#pragma unroll 1
+                        for (int b = 31; b >= 16; --b) {
+                            const float c = key_value(t | (1u << b));
+                            int k = 0;
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) k += (mx[i] >= c) + (mo[i] >= c);
+                            if (k >= need) t |= 1u << b;
+                        }
+                        f = fmaxf(f, key_value(t) - 2.f * bound);
+                    }
                 }
+                if (my_row < n) s_floor[my_row] = f;
             }
-            if (lane == 0) s_floor[t] = f;
+        } else {
+            const int lead_group = (begin - page0) / gp;
+            for (int t = warp; t < n; t += kSelectThreads / 32) {
+                const int stop_t = end_of(t);
+                float f = INFINITY;
+                const float bound = select_bound(s_a[t], *s_max);
+                if (stop_t > begin && bound > 0.f && bound < INFINITY) {
+                    f = -3.4e38f;
+                    if (stop_t - begin > p.cap) {
+                        const float* const mxs = p.maxima + (static_cast<long long>(item) * kSelectTile + t) * row_groups + lead_group;
+                        f = fmaxf(f, border_of((stop_t - page0 + gp - 1) / gp - lead_group, need, [&](int i) { return mxs[i]; }) - 2.f * bound);
+                    }
+                }
+                if (lane == 0) s_floor[t] = f;
+            }
         }
         __syncthreads();
         if (my_row < n) floor = s_floor[my_row];
@@ -486,7 +526,7 @@ __global__ void __launch_bounds__(kSelectThreads, 2) block_filter_kernel(const S
         for (int i = 0; i < 64; ++i) __nanosleep(1000);  // let MMAs in flight drain
     __syncthreads();
     if (my_row < n) {
-        p.counts[list_of(my_row) * 2 + half] = m;
+        p.counts[list_of(my_row) * 2 + half] = static_cast<int>(to_next - found) + m;
         if (half == 0) p.bounds[list_of(my_row)] = select_bound(s_a[my_row], *s_max);
     }
     if (tid == 0) p.bad[item] = *s_abort != 0 ? 3 /* VPP_DEV_TIMEOUT */ : *s_badp ? 2 /* VPP_DEV_BAD_BLOCK */ : 0;
@@ -682,9 +722,9 @@ __global__ void __launch_bounds__(kPickThreads, 4) block_pick_kernel(const Selec
     if (!scan_lengths<kPickThreads>(p.prefix_len, p.chunk_len, p.num_reqs, p.capacity, p.total_q, cu)) return;
     const int G = p.num_q_heads / p.num_kv_heads, need = p.topk - p.num_first - p.num_last;
     PickScratch& s = scratch[warp];
-    const long long rows = static_cast<long long>(p.row1 - p.row0) * p.num_kv_heads, step = static_cast<long long>(work_blocks) * (kPickThreads / 32);
-    for (long long i = static_cast<long long>(blockIdx.x) * (kPickThreads / 32) + warp; i < rows; i += step) {
-        const int t = p.row0 + static_cast<int>(i / p.num_kv_heads), g = static_cast<int>(i % p.num_kv_heads);
+    const int rows = (p.row1 - p.row0) * p.num_kv_heads, step = work_blocks * (kPickThreads / 32);      // (rows of a slab: far below 2^31)
+    for (int i = blockIdx.x * (kPickThreads / 32) + warp; i < rows; i += step) {
+        const int t0 = i / p.num_kv_heads, t = p.row0 + t0, g = i - t0 * p.num_kv_heads;
         const int r = request_of(cu, p.num_reqs, t);
         const int own = (p.prefix_len[r] + (t - cu[r])) >> p.block_shift;
         int32_t* const out = p.indices + (static_cast<long long>(t) * p.num_kv_heads + g) * p.topk;
@@ -700,7 +740,7 @@ __global__ void __launch_bounds__(kPickThreads, 4) block_pick_kernel(const Selec
         float delta = 0.f;
         bool odd = false;
         for (int k = run0 + lane; k < runs; k += 32) {
-            const float x = p.bounds[i * p.runs + k];
+            const float x = p.bounds[static_cast<long long>(i) * p.runs + k];
             odd |= !(x < INFINITY);
             delta = fmaxf(delta, x);
         }
@@ -716,10 +756,10 @@ __global__ void __launch_bounds__(kPickThreads, 4) block_pick_kernel(const Selec
         // the runs' candidates, one behind the other
         int m = 0;
         for (int k = 2 * run0; k < 2 * runs && !odd; ++k) {
-            const int c = p.counts[i * p.runs * 2 + k];
-            odd = c > p.cap || m + c > kPickGather || !(p.bounds[i * p.runs + (k >> 1)] > 0.f);      // (a run whose scores are all 0 lists none)
+            const int c = p.counts[static_cast<long long>(i) * p.runs * 2 + k];
+            odd = c > p.cap || m + c > kPickGather || !(p.bounds[static_cast<long long>(i) * p.runs + (k >> 1)] > 0.f);      // (a run whose scores are all 0 lists none)
             if (odd) break;
-            const SelectCandidate* const from = p.found + (i * p.runs * 2 + k) * p.cap;
+            const SelectCandidate* const from = p.found + (static_cast<long long>(i) * p.runs * 2 + k) * p.cap;
             for (int j = lane; j < c; j += 32) {
                 const SelectCandidate x = from[j];
                 s.score[m + j] = x.score;

@@ -104,7 +104,8 @@ vpp_status select_plan(const vpp_block_select_args* a, SelectPlan* s) {
     const int need = a->topk - a->num_first - a->num_last;
     // A border that is the need-th largest of the maxima of groups lets through about need (1 + need * group / (2 * pages)) pages.  Rows of few pages
     // list them all, others have pages enough for twice as many groups as are needed.
-    s->group_pages = need <= 32 ? 8 : need <= 64 ? 4 : need <= 128 ? 2 : 1;
+    // (Up to 32 are needed: 64 groups, kept in registers.)
+    s->group_pages = need <= 32 ? 0 : need <= 64 ? 4 : need <= 128 ? 2 : 1;
     s->cap = need <= 128 ? 128 : 256;
     auto tiles_of = [&](long long rows) {
         const long long tiles = (rows + N - 1) / N + a->num_reqs;
@@ -120,7 +121,7 @@ vpp_status select_plan(const vpp_block_select_args* a, SelectPlan* s) {
     s->run_pages = static_cast<int>((steps + runs - 1) / runs * N);
     s->runs = static_cast<int>((steps * N + s->run_pages - 1) / s->run_pages);
     const long long list = s->runs * (2ll * s->cap * static_cast<long long>(sizeof(vpp::SelectCandidate)) + 12);     // bytes of a row
-    const long long item = N * (s->run_pages / s->group_pages) * 4;                                                  // of an item
+    const long long item = s->group_pages > 0 ? N * (s->run_pages / s->group_pages) * 4 : 0;                                                  // of an item
     long long slab = vpp::kSelectSlabBytes / (H * (list + item * s->runs / N));
     slab = slab / N * N;                              // (whole tiles of a long chunk)
     if (slab < N) slab = N;
