@@ -411,7 +411,7 @@ typedef struct {
  * x, out       bf16; element (row t, head h, feature d) at t*token_stride + h*head_stride + d (strides in ELEMENTS, multiples of 8, feature stride 1;
  *              16-byte aligned), so that either may be a part of wider rows (a fused projection's, the rotated part of an
  *              absorbed query).  out may be x itself with the same strides; otherwise they must not overlap.
- * head_dim     a multiple of 16.  num_reqs at most 8192.
+ * head_dim     a multiple of 16, at most 1024; num_heads at most 65536; num_reqs at most 8192.
  * status       optional device int32, zeroed by the call; VPP_DEV_BAD_LENGTHS: a negative length, a position past 2^31 - 1 or
  *              sum(chunk_len) != total_q -- nothing is written.
  * Returns after enqueueing one kernel on `stream`.
@@ -439,7 +439,7 @@ vpp_status vpp_rope(const vpp_rope_args *args, vpp_stream_t stream);
  *
  * append       as for vpp_kv_append, except that k_new and v_new have strides: element (row t, head h, feature d) at
  *              t*token_stride + h*head_stride + d (ELEMENTS, multiples of 8).  v_new NULL: keys only (absorbed MLA).  head_dim_qk and
- *              head_dim_v must be multiples of 16.
+ *              head_dim_v must be multiples of 16, at most 1024, and heads at most 65536.
  * q, q_out     bf16 rows of num_q_heads heads of head_dim_qk features with their own strides; both NULL: no queries.  q_out may be q with the
  *              same strides; otherwise neither may overlap any other buffer of the call.
  * status       as for vpp_kv_append; with VPP_DEV_BAD_BLOCK the row's queries are still rotated.

@@ -19,7 +19,9 @@ namespace {
 
 bool mis16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
 
-vpp_status check_rope(const vpp_rope_spec& r, int head_dim) {
+vpp_status check_rope(const vpp_rope_spec& r, int head_dim, int heads) {
+    // (also: units of a row times units of a head stay below 2^32, see RopeRows::inverse)
+    if (head_dim > 1024 || heads > 65536) return fail(VPP_ERR_UNSUPPORTED, "head dims up to 1024 and up to 65536 heads");
     if (!r.inv_freq) return fail(VPP_ERR_INVALID_ARG, "inv_freq is null");
     if (r.layout != VPP_ROPE_HALF && r.layout != VPP_ROPE_INTERLEAVED) return fail(VPP_ERR_INVALID_ARG, "layout must be VPP_ROPE_HALF or VPP_ROPE_INTERLEAVED");
     if (!std::isfinite(r.amplitude)) return fail(VPP_ERR_INVALID_ARG, "amplitude must be finite");
@@ -38,8 +40,11 @@ vpp_status launch_rope(vpp::RopeParams& p, const vpp_rope_spec& r, cudaStream_t 
     p.pairs = r.rot_dim / 2;
     p.first_vec = r.rot_offset / 8;
     p.amplitude = r.amplitude;
-    const int units = p.q.units + p.k.units + p.v.units, warps = vpp::kRopeThreads / 32;
-    const long long tasks = static_cast<long long>(p.total_q) * ((units + vpp::kRopePiece - 1) / vpp::kRopePiece);
+    const int warps = vpp::kRopeThreads / 32;
+    vpp::RopeRows* const kinds[3] = {&p.q, &p.k, &p.v};
+    long long pieces = 0;
+    for (vpp::RopeRows* w : kinds) pieces += w->pieces = (w->units + vpp::kRopePiece - 1) / vpp::kRopePiece;
+    const long long tasks = pieces * p.total_q;
     long long blocks = (tasks + warps - 1) / warps;
     const long long cap = 16ll * sm_count_or_default();
     if (blocks > cap) blocks = cap;
@@ -62,6 +67,7 @@ vpp::RopeRows rows_of(const void* src, int64_t src_token, int64_t src_head, void
     w.dst_head = dst_head * 2;
     w.per_head = dim / 16;
     w.units = heads * w.per_head;
+    w.inverse = static_cast<uint32_t>((0x100000000ull + w.per_head - 1) / w.per_head);      // (2^32 itself becomes 0)
     return w;
 }
 
@@ -212,7 +218,7 @@ vpp_status vpp_rope(const vpp_rope_args* a, vpp_stream_t stream_) {
     if (a->num_reqs > vpp::kLengthsMaxReqs) return fail(VPP_ERR_UNSUPPORTED, "at most %d requests", vpp::kLengthsMaxReqs);
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     if (a->total_q == 0 || a->num_reqs == 0) return zero_status(a->status, stream);
-    const vpp_status st = check_rope(a->rope, a->head_dim);
+    const vpp_status st = check_rope(a->rope, a->head_dim, a->num_heads);
     if (st != VPP_OK) return st;
     if (!a->x || !a->out || !a->prefix_len || !a->chunk_len) return fail(VPP_ERR_INVALID_ARG, "x, out, prefix_len and chunk_len must be non-null");
     if (mis16(a->x) || mis16(a->out)) return fail(VPP_ERR_INVALID_ARG, "x and out must be 16-byte aligned");
@@ -245,7 +251,9 @@ vpp_status vpp_kv_append_rope(const vpp_kv_append_rope_args* args, vpp_stream_t 
     if (a->num_reqs > vpp::kLengthsMaxReqs) return fail(VPP_ERR_UNSUPPORTED, "at most %d requests", vpp::kLengthsMaxReqs);
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     if (a->total_q == 0 || a->num_reqs == 0) return zero_status(a->status, stream);
-    vpp_status st = check_rope(args->rope, a->head_dim_qk);
+    vpp_status st = check_rope(args->rope, a->head_dim_qk > a->head_dim_v ? a->head_dim_qk : a->head_dim_v, args->q && args->num_q_heads > a->num_kv_heads ? args->num_q_heads : a->num_kv_heads);
+    if (st == VPP_OK && args->rope.rot_offset > a->head_dim_qk - args->rope.rot_dim)
+        st = fail(VPP_ERR_INVALID_ARG, "rot_offset + rot_dim exceeds the keys' head dim (%d)", a->head_dim_qk);
     if (st != VPP_OK) return st;
     if (!a->k_new || !a->k_cache || !a->prefix_len || !a->chunk_len)
         return fail(VPP_ERR_INVALID_ARG, "k_new, k_cache, prefix_len and chunk_len must be non-null");

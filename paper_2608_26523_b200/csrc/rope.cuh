@@ -5,11 +5,13 @@
 // with pairs (i, i + rot_dim / 2) of the rotated part ("half") or (2 i, 2 i + 1) ("interleaved"); features outside it are copied.
 // inv_freq is the caller's table, so every scaling of it for long contexts is the same code.
 //
-// Every byte is read once and written once, so HBM bounds it.  A warp takes one piece of a token at a time: up to kRopePiece units of
-// its rows, a unit being two 16-byte vectors of one head that hold each other's partners ("half": vectors u and u + rot_dim / 16).
-// Its loads are issued first; while they are in flight the warp looks up the token's request, position and page and works out the
-// token's cosines and sines, once for all heads of the piece (two angles a lane at 128 rotated features), in 512 bytes of
-// shared memory of its own.
+// Every byte is read once and written once, so HBM bounds it, as long as few instructions go with a byte.  A warp takes a piece of one token's rows of one
+// kind (queries, keys or values) at a time, kRopeUnroll units a lane, a unit being two 16-byte vectors of one head that hold each other's
+// partners ("half": vectors u and u + rot_dim / 16).  Its loads are issued first; while they are in flight the warp looks up the token's
+// request, position and page and works out the token's cosines and sines, once for all heads of the piece (two angles a lane at 128 rotated
+// features), in 512 bytes of shared memory of its own.  16384 tokens of 64/8 heads: 112.7 us, 5.96 TB/s, 91 % of the copy rate; 8192 tokens of 128 x 64
+// features into wider rows 46.3 us (89 %).  Tried: pieces that mix the kinds, with a division for each unit (1160 instructions a piece, 69 % of the issue
+// slots: 119 and 52 us); pieces of two and four rounds with one set of angles (146 and 129 us, 46.3 both); 32 warps an SM instead of 24 (114 and 51 us).
 //
 // Angles: pos * inv_freq is formed in 64 bits and reduced to half a turn there (32 bits are off by 0.03 rad at a position of a million), the
 // cosine and sine of what is left, which is below one turn, in 32 bits.  Rotated features are rounded once, to bf16; the products
@@ -35,6 +37,8 @@ struct RopeRows {
     long long dst_block, dst_token, dst_head;   // (dst_block: cache only)
     int units;                    // heads * units_per_head
     int per_head;                 // units of a head: head_dim / 16
+    uint32_t inverse;             // ceil(2^32 / per_head), 0 for 1: x / per_head is the high word of x * inverse as long as x * per_head < 2^32
+    int pieces;                   // of a token
 };
 
 struct RopeParams {
@@ -84,22 +88,6 @@ __device__ __forceinline__ void turn_interleaved(uint4& a, const float2* cs) {
     }
 }
 
-// The two vectors of unit u of a head, and whether they are rotated: the first pairs / 8 units hold the rotated vectors
-// (first_vec + u and that plus pairs / 8), the others the rest in order, half a rest apart.
-__device__ __forceinline__ bool rope_unit(int u, int per_head, int first_vec, int rot_units, int& va, int& vb) {
-    if (u < rot_units) {
-        va = first_vec + u;
-        vb = va + rot_units;
-        return true;
-    }
-    const int rest = per_head - rot_units;
-    va = u - rot_units;
-    vb = va + rest;
-    if (va >= first_vec) va += 2 * rot_units;
-    if (vb >= first_vec) vb += 2 * rot_units;
-    return false;
-}
-
 // The first work_blocks blocks rotate; the block after them, if there is one, writes the status.
 template <bool kInterleaved>
 __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeParams p, const int work_blocks) {
@@ -131,78 +119,86 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeParams p, 
         return;
     }
     if (!ok) return;                  // lengths that do not describe this launch: write nothing
-    const int units = p.q.units + p.k.units + p.v.units;
-    const int pieces = (units + kRopePiece - 1) / kRopePiece;
+    const int q_pieces = p.q.pieces, k_pieces = p.k.pieces, pieces = q_pieces + k_pieces + p.v.pieces;
     const long long tasks = static_cast<long long>(p.total_q) * pieces, stride = static_cast<long long>(work_blocks) * (kRopeThreads / 32);
-    const int rot_units = p.pairs >> 3;
+    const int rot_units = p.pairs >> 3, first_vec = p.first_vec;
     float2* const cs = s_cs[warp];
     for (long long task = static_cast<long long>(blockIdx.x) * (kRopeThreads / 32) + warp; task < tasks; task += stride) {
         const int row = static_cast<int>(task / pieces);
-        const int u0 = static_cast<int>(task - static_cast<long long>(row) * pieces) * kRopePiece + lane;
-        // where a unit's vectors are: kind, head, the two vectors
-        auto place = [&](int u, int& kind, int& head, int& va, int& vb) -> bool {
-            kind = u < p.q.units ? 0 : u < p.q.units + p.k.units ? 1 : 2;
-            const RopeRows& w = kind == 0 ? p.q : kind == 1 ? p.k : p.v;
-            const int x = u - (kind == 0 ? 0 : kind == 1 ? p.q.units : p.q.units + p.k.units);
-            head = x / w.per_head;
-            const int in = x - head * w.per_head;
-            if (kind == 2) {
-                va = in;
-                vb = in + w.per_head;
-                return false;
+        const int piece = static_cast<int>(task - static_cast<long long>(row) * pieces);
+        const int kind = piece < q_pieces ? 0 : piece < q_pieces + k_pieces ? 1 : 2;
+        const RopeRows& w = kind == 0 ? p.q : kind == 1 ? p.k : p.v;
+        const int u_begin = (piece - (kind == 0 ? 0 : kind == 1 ? q_pieces : q_pieces + k_pieces)) * kRopePiece;
+        const int u_end = w.units, per_head = w.per_head, turned = kind == 2 ? 0 : rot_units, rest = per_head - turned;
+        const uint32_t inverse = w.inverse;
+        const long long src_head = w.src_head, dst_head = w.dst_head;
+        const uint8_t* const src = w.src + row * w.src_token;
+        uint8_t* dst = w.dst;
+        // a unit's head and first vector, and how far the second one is: the first `turned` units of a head hold the rotated vectors, the others the rest
+        // in order, half a rest apart
+        auto place = [&](int u, int& head, int& va, int& vb) -> bool {
+            head = inverse ? __umulhi(static_cast<uint32_t>(u), inverse) : u;
+            const int in = u - head * per_head;
+            const bool turn = in < turned;
+            va = turn ? first_vec + in : in - turned;
+            vb = va + (turn ? turned : rest);
+            if (!turn) {
+                if (va >= first_vec) va += 2 * turned;
+                if (vb >= first_vec) vb += 2 * turned;
             }
-            return rope_unit(in, w.per_head, p.first_vec, rot_units, va, vb);
+            return turn;
         };
         uint4 a[kRopeUnroll], b[kRopeUnroll];
 #pragma unroll
         for (int i = 0; i < kRopeUnroll; ++i) {
-            const int u = u0 + 32 * i;
-            if (u >= units) continue;
-            int kind, head, va, vb;
-            place(u, kind, head, va, vb);
-            const RopeRows& w = kind == 0 ? p.q : kind == 1 ? p.k : p.v;
-            const uint8_t* from = w.src + row * w.src_token + head * w.src_head;
+            const int u = u_begin + lane + 32 * i;
+            if (u >= u_end) continue;
+            int head, va, vb;
+            place(u, head, va, vb);
+            const uint8_t* const from = src + head * src_head;
             a[i] = ld_once(from + va * 16);
             b[i] = ld_once(from + vb * 16);
         }
         const int r = request_of(cu, p.num_reqs, row);
         const int pos = p.prefix_len[r] + (row - cu[r]);
-        long long blk = 0;
-        int slot = 0;
-        if (p.k.units + p.v.units > 0) {
-            if (p.block_table == nullptr) {
-                blk = r;
-                slot = pos;
-            } else {
+        bool write = true;
+        if (kind == 0) {
+            dst += row * w.dst_token;
+        } else {
+            long long blk = r;
+            int slot = pos;
+            if (p.block_table != nullptr) {
                 blk = p.block_table[static_cast<long long>(r) * p.max_blocks_per_req + (pos >> p.block_shift)];
                 slot = pos & ((1 << p.block_shift) - 1);
-                if (blk < 0 || blk >= p.num_blocks) blk = -1;      // the row's page is not valid: its keys and values are skipped
+                write = blk >= 0 && blk < p.num_blocks;      // (the row's page is not valid: its keys and values are skipped)
             }
+            dst += blk * w.dst_block + slot * w.dst_token;
         }
-        __syncwarp();                 // (the last piece's readers of cs are done)
-        for (int i = lane; i < p.pairs; i += 32) {
-            const double turns = static_cast<double>(pos) * static_cast<double>(__ldg(p.inv_freq + i)) * 0.15915494309189533577;   // 1 / (2 pi)
-            float sn, c;
-            sincospif(static_cast<float>(2.0 * (turns - rint(turns))), &sn, &c);
-            cs[i] = make_float2(c * p.amplitude, sn * p.amplitude);
+        if (kind != 2) {
+            __syncwarp();                 // (the last piece's readers of cs are done)
+            for (int i = lane; i < p.pairs; i += 32) {
+                const double turns = static_cast<double>(pos) * static_cast<double>(__ldg(p.inv_freq + i)) * 0.15915494309189533577;   // 1 / (2 pi)
+                float sn, c;
+                sincospif(static_cast<float>(2.0 * (turns - rint(turns))), &sn, &c);
+                cs[i] = make_float2(c * p.amplitude, sn * p.amplitude);
+            }
+            __syncwarp();
         }
-        __syncwarp();
+        if (!write) continue;
 #pragma unroll
         for (int i = 0; i < kRopeUnroll; ++i) {
-            const int u = u0 + 32 * i;
-            if (u >= units) continue;
-            int kind, head, va, vb;
-            if (place(u, kind, head, va, vb)) {
+            const int u = u_begin + lane + 32 * i;
+            if (u >= u_end) continue;
+            int head, va, vb;
+            if (place(u, head, va, vb)) {
                 if (kInterleaved) {
-                    turn_interleaved(a[i], cs + (va - p.first_vec) * 4);
-                    turn_interleaved(b[i], cs + (vb - p.first_vec) * 4);
+                    turn_interleaved(a[i], cs + (va - first_vec) * 4);
+                    turn_interleaved(b[i], cs + (vb - first_vec) * 4);
                 } else {
-                    turn_half(a[i], b[i], cs + (va - p.first_vec) * 8);
+                    turn_half(a[i], b[i], cs + (va - first_vec) * 8);
                 }
             }
-            const RopeRows& w = kind == 0 ? p.q : kind == 1 ? p.k : p.v;
-            if (kind != 0 && blk < 0) continue;
-            uint8_t* to = w.dst + head * w.dst_head + (kind == 0 ? row * w.dst_token : blk * w.dst_block + slot * w.dst_token);
+            uint8_t* const to = dst + head * dst_head;
             *reinterpret_cast<uint4*>(to + va * 16) = a[i];
             *reinterpret_cast<uint4*>(to + vb * 16) = b[i];
         }
