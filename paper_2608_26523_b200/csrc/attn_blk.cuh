@@ -32,7 +32,7 @@
 namespace vpp {
 
 constexpr int kBlkListThreads = 128;
-constexpr int kBlkWindow = 8192;              // mask words of a window of pages
+constexpr int kBlkWindow = 8192;              // mask words of a window of pages, at most
 constexpr int kBlkHalfPages = 4;              // pages of a group's 64 keys, at most (pages of 16)
 
 // One query tile and kv-head.
@@ -56,6 +56,7 @@ struct BlkListParams {
     int total_q, num_kv_heads, topk;
     int tile_tokens, words;       // mask words of a page
     int max_tiles, max_pages;     // tiles of the launch and pages of a union, at most
+    int window;                   // pages whose masks are in shared memory at a time
     WorkHeader* header;           // num_units: tiles; error; counter
     BlkItem* items;               // [Hkv, max_tiles]
     int32_t* pages;               // [Hkv, max_tiles, max_pages]: physical
@@ -64,15 +65,19 @@ struct BlkListParams {
 };
 
 __global__ void __launch_bounds__(kBlkListThreads) block_lists_kernel(const BlkListParams p) {
-    extern __shared__ int32_t cu[];           // cu[num_reqs + 1], then tiles before request r [num_reqs + 1]
-    __shared__ uint32_t s_mask[kBlkWindow];
-    __shared__ int s_count[kBlkListThreads / 32];
+    extern __shared__ int32_t cu[];           // cu[num_reqs + 1], tiles before request r [num_reqs + 1], masks [window, words], pages [window]
+    __shared__ int s_count[kBlkListThreads / 32], s_pages, s_last;
     __shared__ int s_bad;
     int32_t* const first_tile = cu + p.num_reqs + 1;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    if (tid == 0) {
+        s_bad = 0;
+        s_pages = 0;
+        s_last = -1;
+    }
     pdl_launch_dependents();
     pdl_wait();
-    const bool ok = scan_lengths<kBlkListThreads>(p.prefix_len, p.chunk_len, p.num_reqs, p.capacity, p.total_q, cu);
+    const bool ok = scan_lengths<kBlkListThreads>(p.prefix_len, p.chunk_len, p.num_reqs, p.capacity, p.total_q, cu, p.tile_tokens, first_tile);
     if (!ok) {
         if (blockIdx.x == 0 && tid == 0) {
             *p.header = WorkHeader{0, 0, 0, 1 /* VPP_DEV_BAD_LENGTHS */, 0, 0, 0, 0, {}};
@@ -80,8 +85,6 @@ __global__ void __launch_bounds__(kBlkListThreads) block_lists_kernel(const BlkL
         }
         return;
     }
-    if (tid == 0) s_bad = 0;
-    block_scan<kBlkListThreads>(p.num_reqs, 0x7fffffffu, first_tile, false, [&](int r, bool&) { return (cu[r + 1] - cu[r] + p.tile_tokens - 1) / p.tile_tokens; });
     const int tiles = first_tile[p.num_reqs];
     if (blockIdx.x == 0 && tid == 0) {
         *p.header = WorkHeader{tiles, 0, 0, 0, 0, 0, 0, 0, {}};
@@ -99,57 +102,87 @@ __global__ void __launch_bounds__(kBlkListThreads) block_lists_kernel(const BlkL
     const long long item = static_cast<long long>(g) * p.max_tiles + tile;
     int32_t* const pages = p.pages + item * p.max_pages;
     uint2* const masks = p.masks + item * p.max_pages * p.words;
-    const int W = p.words, window = kBlkWindow / W, entries = tokens * p.topk;
-    int count = 0;            // pages so far
-    int last = -1;            // the last of them
-    for (int w0 = 0; w0 < used; w0 += window) {
-        const int n = min(window, used - w0);
-        for (int i = tid; i < n * W; i += kBlkListThreads) s_mask[i] = 0;
-        __syncthreads();
-        for (int i = tid; i < entries; i += kBlkListThreads) {
-            const int t = i / p.topk;
-            const int e = lists[static_cast<long long>(t) * p.num_kv_heads * p.topk + (i - t * p.topk)];
-            if (e >= w0 && e < w0 + n && e <= ((pos0 + t) >> p.block_shift)) atomicOr(&s_mask[(e - w0) * W + (t >> 5)], 1u << (t & 31));
-        }
-        __syncthreads();
-        // a run of pages a warp: count, then write
-        const int run = (n + kBlkListThreads - 1) / kBlkListThreads * 32, a = min(n, warp * run), b = min(n, a + run);
-        auto listed = [&](int i) {
-            uint32_t m = 0;
-            if (i < b)
-                for (int w = 0; w < W; ++w) m |= s_mask[i * W + w];
-            return m != 0;
-        };
-        int mine = 0;
-        for (int i0 = a; i0 < b; i0 += 32) mine += __popc(__ballot_sync(0xffffffffu, listed(i0 + lane)));
-        if (lane == 0) s_count[warp] = mine;
-        __syncthreads();
-        int at = count;
-        for (int w = 0; w < kBlkListThreads / 32; ++w) {
-            if (w < warp) at += s_count[w];
-            count += s_count[w];
-        }
-        for (int i0 = a; i0 < b; i0 += 32) {
-            const int i = i0 + lane;
-            const bool in = listed(i);
-            const uint32_t m = __ballot_sync(0xffffffffu, in);
-            if (in) {
-                const int k = at + __popc(m & ((1u << lane) - 1));
-                const int e = __ldg(table + w0 + i);
-                const bool fine = e >= 0 && e < p.num_blocks;
-                if (!fine) s_bad = 1;
-                pages[k] = fine ? e : p.num_blocks;       // (num_blocks: reads as zero)
-                for (int w = 0; w < W; ++w) masks[static_cast<long long>(k) * W + w] = make_uint2(w0 + i, fine ? s_mask[i * W + w] : 0);
+    const int W = p.words;
+    // Page `e` is the k-th of the union, seen by the tokens of masks word(w).
+    auto put = [&](int k, int e, auto word) {
+        const int phys = __ldg(table + e);
+        const bool fine = phys >= 0 && phys < p.num_blocks;
+        if (!fine) s_bad = 1;
+        pages[k] = fine ? phys : p.num_blocks;       // (num_blocks: reads as zero)
+        for (int w = 0; w < W; ++w) masks[static_cast<long long>(k) * W + w] = make_uint2(e, fine ? word(w) : 0u);
+    };
+    int count = 0;
+    bool done = false;
+    if (tokens == 1) {
+        // A decode row's list, as a selection gives it: ascending, what is no page behind.  It is the union as it is.
+        bool sorted = true;
+        for (int i = tid; i < p.topk; i += kBlkListThreads) {
+            const int e = lists[i], last = i > 0 ? lists[i - 1] : -1, next = i + 1 < p.topk ? lists[i + 1] : -1;
+            const bool valid = e >= 0 && e < used;
+            if (valid && (i > 0 && (last < 0 || last >= e))) sorted = false;
+            if (valid && (next < 0 || next >= used)) {
+                s_pages = i + 1;
+                s_last = e;
             }
-            at += __popc(m);
-            if (m) last = w0 + i0 + 31 - __clz(m);
         }
-        __syncthreads();
+        done = __syncthreads_and(sorted);
+        if (done) {
+            count = s_pages;
+            for (int i = tid; i < count; i += kBlkListThreads) put(i, lists[i], [](int w) { return w == 0 ? 1u : 0u; });
+        }
     }
-    // (the last page of the context is in the last window, in the last run with pages)
+    if (!done) {
+        uint32_t* const s_mask = reinterpret_cast<uint32_t*>(first_tile + p.num_reqs + 1);
+        int32_t* const s_page = reinterpret_cast<int32_t*>(s_mask + p.window * W);
+        const int entries = tokens * p.topk;
+        int last = -1;            // of this warp's pages
+        for (int w0 = 0; w0 < used; w0 += p.window) {
+            const int n = min(p.window, used - w0);
+            for (int i = tid; i < n * W; i += kBlkListThreads) s_mask[i] = 0;
+            __syncthreads();
+            for (int i = tid; i < entries; i += kBlkListThreads) {
+                const int t = i / p.topk;
+                const int e = lists[static_cast<long long>(t) * p.num_kv_heads * p.topk + (i - t * p.topk)];
+                if (e >= w0 && e < w0 + n && e <= ((pos0 + t) >> p.block_shift)) atomicOr(&s_mask[(e - w0) * W + (t >> 5)], 1u << (t & 31));
+            }
+            __syncthreads();
+            // a run of pages a warp: count, then place
+            const int run = (n + kBlkListThreads - 1) / kBlkListThreads * 32, a = min(n, warp * run), b = min(n, a + run);
+            auto listed = [&](int i) {
+                uint32_t m = 0;
+                if (i < b)
+                    for (int w = 0; w < W; ++w) m |= s_mask[i * W + w];
+                return m != 0;
+            };
+            int mine = 0;
+            for (int i0 = a; i0 < b; i0 += 32) mine += __popc(__ballot_sync(0xffffffffu, listed(i0 + lane)));
+            if (lane == 0) s_count[warp] = mine;
+            __syncthreads();
+            int at = 0, found = 0;
+            for (int w = 0; w < kBlkListThreads / 32; ++w) {
+                if (w < warp) at += s_count[w];
+                found += s_count[w];
+            }
+            for (int i0 = a; i0 < b; i0 += 32) {
+                const bool in = listed(i0 + lane);
+                const uint32_t m = __ballot_sync(0xffffffffu, in);
+                if (in) s_page[at + __popc(m & ((1u << lane) - 1))] = i0 + lane;
+                at += __popc(m);
+                if (m) last = w0 + i0 + 31 - __clz(m);
+            }
+            __syncthreads();
+            for (int k = tid; k < found; k += kBlkListThreads) {
+                const int i = s_page[k];
+                put(count + k, w0 + i, [&](int w) { return s_mask[i * W + w]; });
+            }
+            count += found;
+            __syncthreads();
+        }
+        if (lane == 0 && last >= 0) atomicMax(&s_last, last);
+    }
+    __syncthreads();
     const int tail = kv_len & ((1 << p.block_shift) - 1);
-    const int has_last = __syncthreads_or(last == (kv_len - 1) >> p.block_shift);
-    if (tid == 0) p.items[item] = BlkItem{row0, tokens, pos0, count, has_last ? tail : 0, s_bad, {0, 0}};
+    if (tid == 0) p.items[item] = BlkItem{row0, tokens, pos0, count, s_last == (kv_len - 1) >> p.block_shift ? tail : 0, s_bad, {0, 0}};
 }
 
 struct BlkParams {

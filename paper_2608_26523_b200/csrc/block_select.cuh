@@ -153,7 +153,7 @@ __global__ void __launch_bounds__(kSelectThreads, 2) block_filter_kernel(const S
 
     pdl_launch_dependents();
     pdl_wait();
-    const bool ok = scan_lengths<kSelectThreads>(p.prefix_len, p.chunk_len, p.num_reqs, p.capacity, p.total_q, cu);
+    const bool ok = scan_lengths<kSelectThreads>(p.prefix_len, p.chunk_len, p.num_reqs, p.capacity, p.total_q, cu, kSelectTile, first_tile);
     const int item = blockIdx.x;
     if (!ok) {
         if (tid == 0) p.bad[item] = 1 /* VPP_DEV_BAD_LENGTHS */;
@@ -172,10 +172,13 @@ __global__ void __launch_bounds__(kSelectThreads, 2) block_filter_kernel(const S
         mbar_init(bar, 1);
         fence_mbar_init();
     }
-    block_scan<kSelectThreads>(p.num_reqs, 0x7fffffffu, first_tile, false, [&](int r, bool&) {
-        int lo;
-        return (rows_of(r, lo) + kSelectTile - 1) / kSelectTile;
-    });
+    if (p.row0 == 0 && p.row1 == p.total_q)
+        __syncthreads();
+    else                              // (a part of the tokens: tiles begin anew)
+        block_scan<kSelectThreads>(p.num_reqs, 0x7fffffffu, first_tile, false, [&](int r, bool&) {
+            int lo;
+            return (rows_of(r, lo) + kSelectTile - 1) / kSelectTile;
+        });
     const int run = item % p.runs, tg = item / p.runs, g = tg % p.num_kv_heads, tile = tg / p.num_kv_heads;
     if (tile >= first_tile[p.num_reqs]) {
         if (tid == 0) p.bad[item] = 0;

@@ -489,7 +489,9 @@ vpp_status vpp_block_attn_fwd(const vpp_chunk_attn_args* a, const int32_t* block
     lp.pages = reinterpret_cast<int32_t*>(ws + b.pages);
     lp.masks = reinterpret_cast<uint2*>(ws + b.masks);
     lp.status = a->status;
-    const size_t lens = 2 * sizeof(int32_t) * (static_cast<size_t>(a->num_reqs) + 1);
+    const int context = (a->max_seq_len + a->block_size - 1) / a->block_size, most = vpp::kBlkWindow / b.words;
+    lp.window = context < 1 ? 1 : context < most ? context : most;
+    const size_t lens = sizeof(int32_t) * (2 * (static_cast<size_t>(a->num_reqs) + 1) + static_cast<size_t>(lp.window) * (b.words + 1));
     cudaError_t ce = cudaFuncSetAttribute(vpp::block_lists_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lens));
     if (ce == cudaSuccess) ce = cudaFuncSetAttribute(vpp::attn_blk_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, vpp::kBlkSmem);
     if (ce != cudaSuccess) return fail(VPP_ERR_CUDA, "block-sparse attention attributes: %s", cudaGetErrorString(ce));
