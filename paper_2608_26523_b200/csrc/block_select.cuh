@@ -8,16 +8,18 @@
 // The selection is that of exact arithmetic.  Scores are formed in 32 bits with a bound on their error, and where two pages near
 // the border are closer than the bound allows to tell, theirs are formed again in 64 bits (products of bf16 are exact there).
 //
-// Two kernels a slab of tokens (one slab unless their candidates take more than kSelectSlabBytes):
-//  * block_filter_kernel: an item is (up to 128 tokens of one request, kv-head, a run of pages).  The group's queries are
-//    summed first, in 32 bits, and the sum split in two bf16 (hi + rest: 16 bits of it), so that the tensor cores do 2 / group
-//    of the work of all q-heads; scores of 128 tokens x 128 pages are one accumulator.  They are formed twice: the first time the maxima of groups
+// Kernels of a slab of tokens (one slab unless their candidates take more than kSelectSlabBytes):
+//  * block_filter_kernel: an item is (up to 256 tokens of one request, kv-head, a run of pages), a block of 16 warps and one that issues the MMAs.  The group's
+//    queries are summed first, in 32 bits, and the sum split in two bf16 (hi + rest: 16 bits of it), so that the tensor cores do 2 / group
+//    of the work of all q-heads; scores of 128 tokens x 128 pages are one accumulator, and an item has two of those a step, with two buffers: the next step's
+//    products run under this one's scores.  They are formed twice: the first time the maxima of groups
 //    of pages are kept, whose need-th largest bounds a token's border from below; the second time what is not below that by more than the error
 //    bound -- a few more pages than needed -- is written down, a thread a token and half of the pages.  Reading q bounds it (134 MB of
 //    8192 tokens of 64 heads are 21 us; the products twice 4).  (All scores written down once, 4.6 KB a token and kv-head, and picked
-//    from there: 8192 tokens of 64/4 heads with 1152 pages 420 us.)
-//    Items of up to kSelectFew tokens -- decode rows -- take the dot products in registers, half a warp a page, and keep the scores in shared
-//    memory: there reading the means is all.
+//    from there: 8192 tokens of 64/4 heads with 1152 pages 420 us.  Blocks of 128 tokens and eight warps, two an SM, that do one thing after the other: 6500 clk
+//    a step of the two, 115 of 195 us.)
+//  * block_few_kernel: requests of up to kSelectFew tokens -- decode rows -- with the dot products in registers, half a warp a page, and the scores in
+//    shared memory: there reading the means is all.
 //  * block_pick_kernel: a warp a (token, kv-head) ranks the candidates and settles the border.
 #pragma once
 #include <cstdint>
@@ -28,16 +30,21 @@
 
 namespace vpp {
 
-constexpr int kSelectThreads = 256;
-constexpr int kSelectTile = 128;              // tokens of an item, pages of a step
+constexpr int kSelectTile = 128;              // tokens of an accumulator, pages of a step
+constexpr int kSelectItem = 256;              // tokens of an item
+constexpr int kSelectThreads = 512;           // of block_filter_kernel, beside the warp that issues and three that make it a group of four
+// Registers a thread after the roles split: the launch gives 96 (five warps a sub-partition), of which the last four warps hand back 72.
+constexpr int kSelectRegsLow = 24, kSelectRegsHigh = 112;
+static_assert(4 * kSelectRegsHigh + kSelectRegsLow <= 5 * 96, "register budget");
 constexpr int kSelectFew = 4;
+constexpr int kFewThreads = 256;
 constexpr int kSelectSlabBytes = 128 << 20;
 constexpr int kSelectMaxTopk = 256;
-constexpr int kSelectMaxRun = 4096;           // pages of an item: scores of kSelectFew tokens are kept in shared memory
-constexpr int kSelectA = 2 * 2 * kSelectTile * 128;   // two bf16 parts of 128 x 128, two 64-feature slabs each
+constexpr int kSelectMaxRun = 4096;           // pages of an item: scores of kSelectFew tokens, or their places, are kept in shared memory
+constexpr int kSelectA = 2 * 2 * kSelectTile * 128;   // an accumulator's operand: two bf16 parts of 128 x 128, two 64-feature slabs each
 constexpr int kSelectB = 2 * kSelectTile * 128;
-constexpr int kSelectSmem = kSelectA + kSelectB + 1024 /* alignment */ + 2048 /* barrier, borders */;
-static_assert(kSelectFew * kSelectMaxRun * 4 <= kSelectA, "scores of few tokens");
+constexpr int kSelectSmem = 2 * kSelectA + 2 * kSelectB + 1024 /* alignment */ + 4096 /* barriers, borders */;      // and the pages, the lengths
+static_assert(kSelectSmem + 4 * kSelectMaxRun <= 232448 - 8 * 1024, "shared memory of one CTA");
 
 // A page that may be among a token's best.
 struct __align__(8) SelectCandidate {
@@ -62,9 +69,9 @@ struct SelectParams {
     SelectCandidate* found;       // [row1 - row0, Hkv, runs, 2, cap]
     int32_t* counts;              // [row1 - row0, Hkv, runs, 2] (past cap: more than fit)
     float* bounds;                // [row1 - row0, Hkv, runs]: error bound of the row's scores of a run
-    float* maxima;                // [items, 128, run_pages / group_pages] (group_pages > 0)
-    int32_t* bad;                 // one word an item of the slab
-    int items;
+    float* maxima;                // [many_items, 256, run_pages / group_pages] (group_pages > 0)
+    int32_t* bad;                 // one word an item of the slab, of both kernels
+    int many_items, items;        // of block_filter_kernel, of both
     int32_t* indices;             // [total_q, Hkv, topk]
     int32_t* status;
 };
@@ -82,15 +89,35 @@ __device__ __forceinline__ uint32_t abs_max(uint32_t m, uint4 v) {
     }
     return m;
 }
-// |fp32 score - exact score| <= 2^-14 sum_i a_i max|m| + underflow, a_i = sum_h |q_h,i|: the split leaves 2^-17 of the sum, a sum of G
-// terms is off by (G - 1) 2^-24 of a_i (G <= 128), accumulating 256 products by 256 * 2^-23 of their absolute sum: 2^-15, together below 2^-14.  Exactly 0
-// where all products are; infinite or NaN where anything is, or where products could overflow.
-__device__ __forceinline__ float select_bound(float a, uint32_t max_bits) {
-    const float m = __uint_as_float(max_bits << 16);
-    if (!(a < 1e38f)) return INFINITY;
-    if (a == 0.f && max_bits < 0x7f80u) return 0.f;
-    if (max_bits == 0 && a < INFINITY) return 0.f;
-    return a * m * 6.103515625e-5f + 1e-35f;
+// sum of the squares of a vector's features
+__device__ __forceinline__ float square_sum(uint4 v) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    float a = 0.f, b = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        a = fmaf(bf16_lo(w[e]), bf16_lo(w[e]), a);
+        b = fmaf(bf16_hi(w[e]), bf16_hi(w[e]), b);
+    }
+    return a + b;
+}
+// What bounds the error of a run's scores: of the means (one pair a block, by atomicMax of their bits: NaN is above infinity above everything finite) the largest |feature|
+// and the largest sum of a page's squares; of a token the sum of its queries' |features| over the group and the sum of squares of the summed query s.
+//
+//     |fp32 score - exact score| <= c |s| |mean| + G 2^-23 sum|q| max|mean feature|          (|.|: 2-norms)
+//
+// by Cauchy and Schwarz.  c covers forming the product: by the tensor cores 2^-14 (the split leaves 2^-18 of s; 256 products are accumulated with at most 2^-23 of their
+// absolute sum lost each: 2^-15), in registers 2^-19 (8 products and 4 levels of sums of 2^-24).  The second term covers forming s: G - 1 additions of 2^-24 each.
+// Exactly 0 where all products are; infinite or NaN where anything is, or where products could overflow.  (With sum|q| max|mean feature| in place of the norms two thirds of
+// all rows had pages too close to tell, and 8192 tokens of 64/4 heads took 166 us.)
+__device__ __forceinline__ float select_bound(float c, int group, float sum_q, float square_s, uint32_t max_bits, uint32_t square_bits) {
+    const float m = __uint_as_float(max_bits << 16), n2 = __uint_as_float(square_bits);
+    if (!(sum_q < 1e38f)) return INFINITY;
+    if (sum_q == 0.f && max_bits < 0x7f80u) return 0.f;
+    if (max_bits == 0) return 0.f;
+    const float spread = sum_q * m;
+    // (squares that vanish in 32 bits say nothing)
+    const float product = square_s > 1e-30f && n2 > 1e-30f ? sqrtf(square_s) * sqrtf(n2) * 1.001f : spread;
+    return c * product + static_cast<float>(group) * 1.1920929e-7f * spread + 1e-35f;
 }
 
 // Unsigned integers in the order of floats; NaN below everything.
@@ -133,86 +160,44 @@ __device__ __forceinline__ float border_of(int n, int need, Value value) {
     return need <= 64 ? border_below<8>(n, need, value) : border_below<16>(n, need, value);
 }
 
-__global__ void __launch_bounds__(kSelectThreads, 2) block_filter_kernel(const SelectParams p) {
-    extern __shared__ uint8_t smem_raw[];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    uint8_t* const gen = smem_raw + (base - smem_u32(smem_raw));
-    uint8_t* const sA = gen;
-    uint8_t* const sB = gen + kSelectA;
-    uint8_t* const sX = gen + kSelectA + kSelectB;
-    const uint32_t bar = base + kSelectA + kSelectB;
-    volatile int* const s_abort = reinterpret_cast<volatile int*>(sX + 8);
-    volatile uint32_t* const s_tmem = reinterpret_cast<volatile uint32_t*>(sX + 12);
-    uint32_t* const s_max = reinterpret_cast<uint32_t*>(sX + 16);
-    int* const s_badp = reinterpret_cast<int*>(sX + 20);
-    float* const s_a = reinterpret_cast<float*>(sX + 32);              // [128] what a bound is made of
-    float* const s_floor = reinterpret_cast<float*>(sX + 32 + 512);    // [128] lowest score of a candidate
-    int32_t* const cu = reinterpret_cast<int32_t*>(sX + 2048);         // [num_reqs + 1], then tile counts [num_reqs + 1]
-    int32_t* const first_tile = cu + p.num_reqs + 1;
+// Rows of request r inside the slab: their number, and the first.
+__device__ __forceinline__ int slab_rows(const SelectParams& p, const int32_t* cu, int r, int& lo) {
+    lo = max(cu[r], p.row0);
+    const int n = min(cu[r + 1], p.row1) - lo;
+    return n > 0 ? n : 0;
+}
 
+// Requests of few tokens (with few_only set, of any number, kSelectFew at a time): a block a (request, kv-head, run of pages).
+__global__ void __launch_bounds__(kFewThreads) block_few_kernel(const SelectParams p, const int few_only) {
+    extern __shared__ float s_score[];                              // [kSelectFew][run_pages], then cu [num_reqs + 1]
+    __shared__ uint32_t s_max, s_square;
+    __shared__ int s_bad;
+    int32_t* const cu = reinterpret_cast<int32_t*>(s_score + kSelectFew * p.run_pages);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, v = tid & 15;
+    if (tid == 0) s_bad = 0;
     pdl_launch_dependents();
     pdl_wait();
-    const bool ok = scan_lengths<kSelectThreads>(p.prefix_len, p.chunk_len, p.num_reqs, p.capacity, p.total_q, cu, kSelectTile, first_tile);
-    const int item = blockIdx.x;
-    if (!ok) {
-        if (tid == 0) p.bad[item] = 1 /* VPP_DEV_BAD_LENGTHS */;
-        return;
-    }
-    // tiles of every request's rows inside the slab
-    auto rows_of = [&](int r, int& lo) {
-        lo = max(cu[r], p.row0);
-        const int n = min(cu[r + 1], p.row1) - lo;
-        return n > 0 ? n : 0;
-    };
-    if (tid == 0) {
-        *s_abort = 0;
-        *s_max = 0;
-        *s_badp = 0;
-        mbar_init(bar, 1);
-        fence_mbar_init();
-    }
-    if (p.row0 == 0 && p.row1 == p.total_q)
-        __syncthreads();
-    else                              // (a part of the tokens: tiles begin anew)
-        block_scan<kSelectThreads>(p.num_reqs, 0x7fffffffu, first_tile, false, [&](int r, bool&) {
-            int lo;
-            return (rows_of(r, lo) + kSelectTile - 1) / kSelectTile;
-        });
-    const int run = item % p.runs, tg = item / p.runs, g = tg % p.num_kv_heads, tile = tg / p.num_kv_heads;
-    if (tile >= first_tile[p.num_reqs]) {
-        if (tid == 0) p.bad[item] = 0;
-        return;
-    }
-    const int r = request_of(first_tile, p.num_reqs, tile);
+    const bool ok = scan_lengths<kFewThreads>(p.prefix_len, p.chunk_len, p.num_reqs, p.capacity, p.total_q, cu);
+    int32_t* const flag = p.bad + p.many_items + blockIdx.x;
+    const int run = blockIdx.x % p.runs, rg = blockIdx.x / p.runs, g = rg % p.num_kv_heads, r = rg / p.num_kv_heads;
     int lo;
-    const int rows_r = rows_of(r, lo);
-    const int row = lo + (tile - first_tile[r]) * kSelectTile;
-    const int n = min(kSelectTile, lo + rows_r - row);
-    const int pos0 = p.prefix_len[r] + (row - cu[r]);
-    const int end = select_end(p, (pos0 + n - 1) >> p.block_shift);      // of the tile's last token
-    // a page run that nobody needs: below the first candidate, past the last, or no token has more pages than it may list
-    const int page0 = run * p.run_pages, page1 = min(page0 + p.run_pages, end), begin = max(page0, p.num_first);
-    if (page1 <= begin || ((pos0 + n - 1) >> p.block_shift) + 1 <= p.topk) {
-        if (tid == 0) p.bad[item] = 0;
+    const int rows = ok ? slab_rows(p, cu, r, lo) : 0;
+    if (rows == 0 || (rows > kSelectFew && !few_only)) {
+        if (tid == 0) *flag = ok ? 0 : 1 /* VPP_DEV_BAD_LENGTHS */;
         return;
     }
     const int G = p.num_q_heads / p.num_kv_heads, need = p.topk - p.num_first - p.num_last;
     const int32_t* const table = p.block_table + static_cast<long long>(r) * p.max_blocks_per_req;
-    const uint8_t* const q0 = p.q + (static_cast<long long>(row) * p.num_q_heads + g * G) * 256;
-    // of token t of the tile: candidates of this run (one past the last), and where its lists are
-    auto end_of = [&](int t) {
-        const int own = (pos0 + t) >> p.block_shift;
-        return own + 1 <= p.topk ? 0 : min(page1, select_end(p, own));
-    };
-    auto list_of = [&](int t) { return (static_cast<long long>(row - p.row0 + t) * p.num_kv_heads + g) * p.runs + run; };
-    const int v = tid & 15;
     bool bad = false;
-    uint32_t top = 0;
-
-    if (n <= kSelectFew) {
-        // ---- a few tokens: half a warp a page ----
-        float* const s_score = reinterpret_cast<float*>(sA);       // [kSelectFew][run_pages]
+    for (int row = lo; row < lo + rows; row += kSelectFew) {
+        const int n = min(kSelectFew, lo + rows - row), pos0 = p.prefix_len[r] + (row - cu[r]);
+        const int end = select_end(p, (pos0 + n - 1) >> p.block_shift);      // of the last token
+        // a page run that nobody needs: below the first candidate, past the last, or no token has more pages than it may list
+        const int page0 = run * p.run_pages, page1 = min(page0 + p.run_pages, end), begin = max(page0, p.num_first);
+        if (page1 <= begin || ((pos0 + n - 1) >> p.block_shift) + 1 <= p.topk) continue;
+        __syncthreads();                  // (the last round's scores are read)
+        if (tid == 0) s_max = s_square = 0;
+        const uint8_t* const q0 = p.q + (static_cast<long long>(row) * p.num_q_heads + g * G) * 256;
         float s[kSelectFew][8], a[kSelectFew];
 #pragma unroll
         for (int t = 0; t < kSelectFew; ++t) {
@@ -236,13 +221,15 @@ __global__ void __launch_bounds__(kSelectThreads, 2) block_filter_kernel(const S
 #pragma unroll
             for (int o = 8; o > 0; o >>= 1) a[t] += __shfl_xor_sync(0xffffffffu, a[t], o);
         }
-        constexpr int kDeep = 8, kStep = kDeep * (kSelectThreads / 16);
+        constexpr int kDeep = 8, kStep = kDeep * (kFewThreads / 16);
         const int half = tid >> 4;
+        uint32_t top = 0;
+        float square = 0.f;
         int e[kDeep];
         auto look = [&](int j0) {
 #pragma unroll
             for (int i = 0; i < kDeep; ++i) {
-                const int j = j0 + i * (kSelectThreads / 16) + half;
+                const int j = j0 + i * (kFewThreads / 16) + half;
                 e[i] = j < page1 ? __ldg(table + j) : 0;
             }
         };
@@ -251,17 +238,21 @@ __global__ void __launch_bounds__(kSelectThreads, 2) block_filter_kernel(const S
             uint4 x[kDeep];
 #pragma unroll
             for (int i = 0; i < kDeep; ++i) {
-                const int j = j0 + i * (kSelectThreads / 16) + half;
+                const int j = j0 + i * (kFewThreads / 16) + half;
                 const bool fine = e[i] >= 0 && e[i] < p.num_blocks;
                 bad |= !fine;
-                x[i] = make_uint4(0, 0, 0, 0);
+                x[i] = make_uint4(0, 0, 0, 0);        // (pages that are taken anyway count as 0: what theirs hold must not widen the bound)
                 if (j < page1 && j >= begin && fine) x[i] = ld_once(p.means + (static_cast<long long>(e[i]) * p.num_kv_heads + g) * 256 + v * 16);
             }
             look(j0 + kStep);
 #pragma unroll
             for (int i = 0; i < kDeep; ++i) {
-                const int j = j0 + i * (kSelectThreads / 16) + half;
+                const int j = j0 + i * (kFewThreads / 16) + half;
                 top = abs_max(top, x[i]);
+                float sq = square_sum(x[i]);
+#pragma unroll
+                for (int o = 8; o > 0; o >>= 1) sq += __shfl_xor_sync(0xffffffffu, sq, o);
+                square = sq > square || !(sq == sq) ? sq : square;      // (NaN stays)
                 const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
 #pragma unroll
                 for (int t = 0; t < kSelectFew; ++t) {
@@ -278,241 +269,403 @@ __global__ void __launch_bounds__(kSelectThreads, 2) block_filter_kernel(const S
                 }
             }
         }
+        __syncthreads();                  // (s_max is 0)
         top = __reduce_max_sync(0xffffffffu, top);
-        if (lane == 0) atomicMax(s_max, top);
-        if (bad) *s_badp = 1;
+        const uint32_t warp_square = __reduce_max_sync(0xffffffffu, __float_as_uint(square) & 0x7fffffffu);
+        if (lane == 0) {
+            atomicMax(&s_max, top);
+            atomicMax(&s_square, warp_square);
+        }
         __syncthreads();
-        if (warp < n) {
-            float at = a[0];
+        if (warp >= n) continue;
+        float at = 0.f, ss = 0.f;
 #pragma unroll
-            for (int t = 1; t < kSelectFew; ++t)
-                if (warp == t) at = a[t];
-            const float bound = select_bound(at, *s_max);
-            const int stop = end_of(warp);
-            const long long list = list_of(warp);
-            const float* const mine = s_score + warp * p.run_pages - page0;
-            if (lane == 0) p.bounds[list] = bound;
-            int m = 0;
-            if (bound > 0.f && bound < INFINITY && stop > begin) {
-                const float floor = stop - begin <= p.cap ? -INFINITY : border_of(stop - begin, need, [&](int i) { return mine[begin + i]; }) - 2.f * bound;
-                SelectCandidate* const found = p.found + list * 2 * p.cap;
-                for (int j0 = begin; j0 < stop; j0 += 32) {
-                    const int j = j0 + lane;
-                    const float x = j < stop ? mine[j] : 0.f;
-                    const bool take = j < stop && x >= floor;
-                    const uint32_t b = __ballot_sync(0xffffffffu, take);
-                    const int at_m = m + __popc(b & ((1u << lane) - 1));
-                    if (take && at_m < p.cap) found[at_m] = SelectCandidate{x, j};
-                    m += __popc(b);
-                }
+        for (int t = 0; t < kSelectFew; ++t)
+            if (warp == t) {
+                at = a[t];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) ss = fmaf(s[t][k], s[t][k], ss);
             }
-            if (lane == 0) {
-                p.counts[list * 2] = m;
-                p.counts[list * 2 + 1] = 0;
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+        const float bound = select_bound(1.9073486e-6f /* 2^-19 */, G, at, ss, s_max, s_square);
+        const int own = (pos0 + warp) >> p.block_shift, stop = own + 1 <= p.topk ? 0 : min(page1, select_end(p, own));
+        const long long list = (static_cast<long long>(row - p.row0 + warp) * p.num_kv_heads + g) * p.runs + run;
+        const float* const mine = s_score + warp * p.run_pages - page0;
+        int m = 0;
+        if (bound > 0.f && bound < INFINITY && stop > begin) {
+            const float floor = stop - begin <= p.cap ? -INFINITY : border_of(stop - begin, need, [&](int i) { return mine[begin + i]; }) - 2.f * bound;
+            SelectCandidate* const found = p.found + list * 2 * p.cap;
+            for (int j0 = begin; j0 < stop; j0 += 32) {
+                const int j = j0 + lane;
+                const float x = j < stop ? mine[j] : 0.f;
+                const bool take = j < stop && x >= floor;
+                const uint32_t b = __ballot_sync(0xffffffffu, take);
+                const int at_m = m + __popc(b & ((1u << lane) - 1));
+                if (take && at_m < p.cap) found[at_m] = SelectCandidate{x, j};
+                m += __popc(b);
             }
         }
-        if (tid == 0) p.bad[item] = *s_badp ? 2 /* VPP_DEV_BAD_BLOCK */ : 0;
+        if (lane == 0) {
+            p.bounds[list] = bound;
+            p.counts[list * 2] = m;
+            p.counts[list * 2 + 1] = 0;
+        }
+    }
+    if (bad) s_bad = 1;
+    __syncthreads();
+    if (tid == 0) *flag = s_bad ? 2 /* VPP_DEV_BAD_BLOCK */ : 0;
+}
+
+__global__ void __launch_bounds__(kSelectThreads + 128, 1) block_filter_kernel(const SelectParams p) {
+    extern __shared__ uint8_t smem_raw[];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    uint8_t* const gen = smem_raw + (base - smem_u32(smem_raw));
+    uint8_t* const sB = gen + 2 * kSelectA;
+    uint8_t* const sX = sB + 2 * kSelectB;
+    const uint32_t bar = base + 2 * kSelectA + 2 * kSelectB;           // [2] scores of a buffer
+    volatile int* const s_abort = reinterpret_cast<volatile int*>(sX + 16);
+    volatile uint32_t* const s_tmem = reinterpret_cast<volatile uint32_t*>(sX + 20);
+    uint32_t* const s_max = reinterpret_cast<uint32_t*>(sX + 24);
+    int* const s_badp = reinterpret_cast<int*>(sX + 28);
+    uint32_t* const s_square = reinterpret_cast<uint32_t*>(sX + 32);
+    float* const s_a = reinterpret_cast<float*>(sX + 64);              // [256] what a bound is made of: sum of |q|
+    float* const s_ss = s_a + kSelectItem;                             // [256] and the summed query's squares
+    float* const s_floor = s_ss + kSelectItem;                         // [256] lowest score of a candidate
+    int32_t* const s_page = reinterpret_cast<int32_t*>(sX + 4096);     // [run_pages] physical page, -1: counts as 0
+    int32_t* const cu = s_page + p.run_pages;                          // [num_reqs + 1], then items before request r [num_reqs + 1]
+    int32_t* const first_item = cu + p.num_reqs + 1;
+
+    if (tid == 0) {
+        *s_abort = 0;
+        *s_max = 0;
+        *s_square = 0;
+        *s_badp = 0;
+        mbar_init(bar, 1);
+        mbar_init(bar + 8, 1);
+        fence_mbar_init();
+    }
+    pdl_launch_dependents();
+    pdl_wait();
+    constexpr int kAll = kSelectThreads + 128;
+    const bool ok = scan_lengths<kAll>(p.prefix_len, p.chunk_len, p.num_reqs, p.capacity, p.total_q, cu);
+    const int item = blockIdx.x;
+    if (!ok) {
+        if (tid == 0) p.bad[item] = 1 /* VPP_DEV_BAD_LENGTHS */;
         return;
     }
-
-    // ---- many tokens: tensor cores ----
-    if (warp == 0) {
-        tmem_alloc(smem_u32(const_cast<uint32_t*>(s_tmem)), 128);
+    block_scan<kAll>(p.num_reqs, 0x7fffffffu, first_item, false, [&](int r, bool&) {
+        int lo;
+        const int n = slab_rows(p, cu, r, lo);
+        return n > kSelectFew ? (n + kSelectItem - 1) / kSelectItem : 0;      // (the others: block_few_kernel)
+    });
+    const int run = item % p.runs, tg = item / p.runs, g = tg % p.num_kv_heads, tile = tg / p.num_kv_heads;
+    if (tile >= first_item[p.num_reqs]) {
+        if (tid == 0) p.bad[item] = 0;
+        return;
+    }
+    const int r = request_of(first_item, p.num_reqs, tile);
+    int lo;
+    const int rows_r = slab_rows(p, cu, r, lo);
+    const int row = lo + (tile - first_item[r]) * kSelectItem;
+    const int n = min(kSelectItem, lo + rows_r - row);
+    const int pos0 = p.prefix_len[r] + (row - cu[r]);
+    const int end = select_end(p, (pos0 + n - 1) >> p.block_shift);      // of the item's last token
+    // a page run that nobody needs: below the first candidate, past the last, or no token has more pages than it may list
+    const int page0 = run * p.run_pages, page1 = min(page0 + p.run_pages, end), begin = max(page0, p.num_first);
+    if (page1 <= begin || ((pos0 + n - 1) >> p.block_shift) + 1 <= p.topk) {
+        if (tid == 0) p.bad[item] = 0;
+        return;
+    }
+    const int G = p.num_q_heads / p.num_kv_heads, need = p.topk - p.num_first - p.num_last, pages = page1 - page0;
+    // of token t of the item: candidates of this run (one past the last), and where its lists are
+    auto end_of = [&](int t) {
+        const int own = (pos0 + t) >> p.block_shift;
+        return own + 1 <= p.topk ? 0 : min(page1, select_end(p, own));
+    };
+    auto list_of = [&](int t) { return (static_cast<long long>(row - p.row0 + t) * p.num_kv_heads + g) * p.runs + run; };
+    if (warp == kSelectThreads / 32) {
+        tmem_alloc(smem_u32(const_cast<uint32_t*>(s_tmem)), 512);
         tmem_relinquish();
     }
-    uint4 x[8];
-    int e[8];
-    auto look = [&](int j0) {         // pages of the thread's eight vectors, rows tid / 16 + 16 i of the step
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int j = j0 + (tid >> 4) + 16 * i;
-            e[i] = j < page1 ? __ldg(table + j) : 0;
-        }
-    };
-    auto fetch = [&](int j0) {        // their means
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int j = j0 + (tid >> 4) + 16 * i;
-            const bool fine = e[i] >= 0 && e[i] < p.num_blocks;
+    {
+        const int32_t* const table = p.block_table + static_cast<long long>(r) * p.max_blocks_per_req + page0;
+        bool bad = false;
+        for (int j = tid; j < pages; j += kAll) {
+            const int e = __ldg(table + j);
+            const bool fine = e >= 0 && e < p.num_blocks;
             bad |= !fine;
-            x[i] = make_uint4(0, 0, 0, 0);        // (pages that are taken anyway count as 0: what theirs hold must not widen the bound)
-            if (j < page1 && j >= begin && fine) x[i] = ld_once(p.means + (static_cast<long long>(e[i]) * p.num_kv_heads + g) * 256 + v * 16);
+            s_page[j] = fine && page0 + j >= begin ? e : -1;      // (pages that are taken anyway count as 0: what theirs hold must not widen the bound)
         }
-    };
-    look(page0);
-    for (int t = tid >> 4; t < n; t += kSelectThreads / 16) {
-        float s[8] = {}, a = 0.f;
-        const uint8_t* src = q0 + static_cast<long long>(t) * p.num_q_heads * 256 + v * 16;
+        if (bad) *s_badp = 1;
+    }
+    const int v = tid & 15;
+    // ---- the group's queries, summed and split ----
+    if (tid < kSelectThreads) {
+        const uint8_t* const q0 = p.q + (static_cast<long long>(row) * p.num_q_heads + g * G) * 256 + v * 16;
+        for (int t = tid >> 4; t < n; t += kSelectThreads / 16) {
+            float s[8] = {}, a = 0.f;
+            const uint8_t* const src = q0 + static_cast<long long>(t) * p.num_q_heads * 256;
 #pragma unroll 8
-        for (int h = 0; h < G; ++h) {
-            const uint4 y = ld_once(src + h * 256);
-            const uint32_t w[4] = {y.x, y.y, y.z, y.w};
+            for (int h = 0; h < G; ++h) {
+                const uint4 y = ld_once(src + h * 256);
+                const uint32_t w[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    s[2 * k] += bf16_lo(w[k]);
+                    s[2 * k + 1] += bf16_hi(w[k]);
+                    a += fabsf(bf16_lo(w[k])) + fabsf(bf16_hi(w[k]));
+                }
+            }
+            const unsigned half_mask = 0xffffu << (lane & 16);        // (the other half's token may not exist)
+            float ss = 0.f;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) ss = fmaf(s[k], s[k], ss);
+#pragma unroll
+            for (int o = 8; o > 0; o >>= 1) {
+                a += __shfl_xor_sync(half_mask, a, o);
+                ss += __shfl_xor_sync(half_mask, ss, o);
+            }
+            uint32_t hi[4], rest[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                s[2 * k] += bf16_lo(w[k]);
-                s[2 * k + 1] += bf16_hi(w[k]);
-                a += fabsf(bf16_lo(w[k])) + fabsf(bf16_hi(w[k]));
+                hi[k] = pack_bf16x2(s[2 * k], s[2 * k + 1]);
+                rest[k] = pack_bf16x2(s[2 * k] - bf16_lo(hi[k]), s[2 * k + 1] - bf16_hi(hi[k]));
+            }
+            uint8_t* const to = gen + (t >> 7) * kSelectA + (v >> 3) * (kSelectTile * 128) + (t & 127) * 128 + (((v & 7) ^ (t & 7)) << 4);
+            *reinterpret_cast<uint4*>(to) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+            *reinterpret_cast<uint4*>(to + kSelectA / 2) = make_uint4(rest[0], rest[1], rest[2], rest[3]);
+            if (v == 0) {
+                s_a[t] = a;
+                s_ss[t] = ss;
             }
         }
-        const unsigned half_mask = 0xffffu << (lane & 16);        // (the other half's token may not exist)
-#pragma unroll
-        for (int o = 8; o > 0; o >>= 1) a += __shfl_xor_sync(half_mask, a, o);
-        uint32_t hi[4], rest[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            hi[k] = pack_bf16x2(s[2 * k], s[2 * k + 1]);
-            rest[k] = pack_bf16x2(s[2 * k] - bf16_lo(hi[k]), s[2 * k + 1] - bf16_hi(hi[k]));
-        }
-        uint8_t* const to = sA + (v >> 3) * (kSelectTile * 128) + t * 128 + (((v & 7) ^ (t & 7)) << 4);
-        *reinterpret_cast<uint4*>(to) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-        *reinterpret_cast<uint4*>(to + kSelectA / 2) = make_uint4(rest[0], rest[1], rest[2], rest[3]);
-        if (v == 0) s_a[t] = a;
     }
-    fetch(page0);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *s_tmem;
-    constexpr uint32_t kIdesc = idesc_bf16(kSelectTile, kSelectTile, false, false), kHi = desc_hi_sw128(1024);
-    const int my_row = (warp & 3) * 32 + lane, half = warp >> 2;
+    // no more candidates than fit: no border is needed, one pass over the pages is enough
+    const bool filter = page1 - begin > p.cap;
+    const int per_pass = (pages + kSelectTile - 1) / kSelectTile, steps = filter ? 2 * per_pass : per_pass;
+    auto first_page = [&](int j) { return (j >= per_pass ? j - per_pass : j) * kSelectTile; };      // (counted from page0)
+
+    if (tid >= kSelectThreads) {
+        // ============================ MMA issuer ============================
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kSelectRegsLow));
+        constexpr uint32_t kIdesc = idesc_bf16(kSelectTile, kSelectTile, false, false), kHi = desc_hi_sw128(1024);
+        for (int j = 0; j < steps; ++j) {
+            __syncthreads();              // step j's operand is in place, and the scores of two steps ago have left tensor memory
+            if (tid == kSelectThreads) {
+                tc_fence_after();
+                const uint32_t b0 = desc_lo_sw128(base + 2 * kSelectA + (j & 1) * kSelectB, 16);
+                for (int t = 0; t * kSelectTile < n; ++t) {
+                    const uint32_t a0 = desc_lo_sw128(base + t * kSelectA, 16);
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) {
+                        const uint32_t at = (((k >> 2) & 1) * (kSelectTile * 128) + (k & 3) * 32) >> 4;
+                        mma_ss_lhh(tmem + (j & 1) * 256 + t * 128, a0 + (k >> 3) * (kSelectA / 2 >> 4) + at, kHi, b0 + at, kHi, kIdesc, k > 0);
+                    }
+                }
+                tc_commit(bar + 8 * (j & 1));
+            }
+            __syncwarp();
+            if (filter && j == per_pass) {      // (with the borders: see below)
+                __syncthreads();
+                __syncthreads();
+            }
+        }
+        __syncthreads();
+        __syncthreads();
+        if (warp == kSelectThreads / 32) tmem_dealloc(tmem, 512);
+        return;
+    }
+    // ============================ the others: operands, scores ============================
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSelectRegsHigh));
+    uint32_t top = 0, square = 0;
+    auto bound_of = [&](int t) { return select_bound(6.1035156e-5f /* 2^-14 */, G, s_a[t], s_ss[t], *s_max, *s_square); };
+    auto share_bounds = [&]() {           // the means' part, before a barrier
+        const uint32_t a = __reduce_max_sync(0xffffffffu, top), b = __reduce_max_sync(0xffffffffu, square);
+        if (lane == 0) {
+            atomicMax(s_max, a);
+            atomicMax(s_square, b);
+        }
+    };
+    // The thread's four vectors of the means of step j, of rows tid / 16 + 32 i, on the way into the operand's place; zeros where there is no page.
+    auto place_of = [&](int j, int i) -> uint32_t {
+        const int t = (tid >> 4) + 32 * i;
+        return (j & 1) * kSelectB + (v >> 3) * (kSelectTile * 128) + t * 128 + (((v & 7) ^ (t & 7)) << 4);
+    };
+    const uint8_t* const my_means = p.means + g * 256 + v * 16;
+    const long long mean_stride = static_cast<long long>(p.num_kv_heads) * 256;
+    auto fetch = [&](int j) {
+        if (j < steps) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int k = first_page(j) + (tid >> 4) + 32 * i;
+                const int e = k < pages ? s_page[k] : -1;
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(base + 2 * kSelectA + place_of(j, i)), "l"(my_means + max(e, 0) * mean_stride),
+                             "r"(e >= 0 ? 16 : 0) : "memory");
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    auto landed = [&](int j) {            // the thread's own copies of step j are done, and seen by the tensor core after the barrier that follows
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        if (j < per_pass) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint4 x = *reinterpret_cast<const uint4*>(sB + place_of(j, i));
+                top = abs_max(top, x);
+                float sq = square_sum(x);
+#pragma unroll
+                for (int o = 8; o > 0; o >>= 1) sq += __shfl_xor_sync(0xffffffffu, sq, o);
+                square = max(square, __float_as_uint(sq) & 0x7fffffffu);
+            }
+        }
+        fence_proxy_async_smem();
+    };
+    // warps 0-3 and 4-7: the first 128 tokens, left and right halves of a step's pages; warps 8-15: the other tokens
+    const int my_row = (warp >> 3) * 128 + (warp & 3) * 32 + lane, half = (warp >> 2) & 1;
+    const uint32_t tD = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + (warp >> 3) * 128 + half * 64;
+    const bool tile_lives = (warp >> 3) * 128 < n;
     const int stop = my_row < n ? end_of(my_row) : 0;
     const int gp = p.group_pages, row_groups = gp > 0 ? p.run_pages / gp : 0;
-    float* const my_maxima = p.maxima + (static_cast<long long>(item) * kSelectTile + my_row) * row_groups;
-    // no more candidates than fit: no border is needed
-    const bool filter = page1 - begin > p.cap;
-    uint32_t phase = 0;
-    bool alive = true;
+    float* const my_maxima = p.maxima + (static_cast<long long>(item) * kSelectItem + my_row) * row_groups;
     float floor = -3.4e38f;      // (below every score that counts and above the -inf of pages that are no candidates)
-    SelectCandidate* const found = p.found + (list_of(my_row) * 2 + half) * p.cap;
-    SelectCandidate* to_next = found;
+    // (a slab's lists are far below 4 GB: offsets of 32 bits, one instruction to move on)
+    const uint32_t list0 = static_cast<uint32_t>((list_of(my_row) * 2 + half) * p.cap * sizeof(SelectCandidate)), list_room = p.cap * sizeof(SelectCandidate);
+    uint32_t put_at = list0;
+    auto put = [&](float score, int page) {
+        *reinterpret_cast<SelectCandidate*>(reinterpret_cast<uint8_t*>(p.found) + put_at) = SelectCandidate{score, page};
+        put_at += sizeof(SelectCandidate);
+    };
     int m = 0;                   // those that found no room
     float mx[32];                // gp == 0: of the pages that are column i of a piece
 #pragma unroll
     for (int i = 0; i < 32; ++i) mx[i] = -INFINITY;
-    for (int pass = filter ? 0 : 1; pass < 2 && alive; ++pass) {
-        for (int j0 = page0; j0 < page1; j0 += kSelectTile) {
-            const bool more = j0 + kSelectTile < page1;
-            if (more || pass == 0) look(more ? j0 + kSelectTile : page0);
+    fetch(0);
+    landed(0);
+    __syncthreads();
+    fetch(1);
+    bool alive = true;
+    for (int j = 0; j < steps; ++j) {
+        if (j + 1 < steps) {
+            landed(j + 1);
+            __syncthreads();
+        }
+        if (alive) alive = mbar_wait(bar + 8 * (j & 1), (j >> 1) & 1, s_abort, 501);
+        // (this step's products have read their operand: the one after next goes to its place -- after the borders, which pass through it)
+        const bool borders = filter && j == per_pass - 1;
+        if (!borders) fetch(j + 2);
+        const bool first_pass = filter && j < per_pass;
+        tc_fence_after();
+        if (alive && tile_lives) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int t = (tid >> 4) + 16 * i;
-                if (pass == 0 || !filter) top = abs_max(top, x[i]);
-                *reinterpret_cast<uint4*>(sB + (v >> 3) * (kSelectTile * 128) + t * 128 + (((v & 7) ^ (t & 7)) << 4)) = x[i];
-            }
-            fence_proxy_async_smem();
-            __syncthreads();              // (operands in place; the last step's scores have left tensor memory)
-            if (tid == 0) {
-                tc_fence_after();
-                const uint32_t a0 = desc_lo_sw128(base, 16), b0 = desc_lo_sw128(base + kSelectA, 16);
-#pragma unroll
-                for (int k = 0; k < 16; ++k) {
-                    const uint32_t at = (((k >> 2) & 1) * (kSelectTile * 128) + (k & 3) * 32) >> 4;
-                    mma_ss_lhh(tmem, a0 + (k >> 3) * (kSelectA / 2 >> 4) + at, kHi, b0 + at, kHi, kIdesc, k > 0);
-                }
-                tc_commit(bar);
-            }
-            if (more || pass == 0) fetch(more ? j0 + kSelectTile : page0);
-            alive = __syncthreads_and(mbar_wait(bar, phase, s_abort, 501));
-            if (!alive) break;
-            phase ^= 1;
-            tc_fence_after();
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                uint32_t s[32];
-                tmem_ld32(tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + half * 64 + c * 32, s);
+            for (int c = 0; c < 4; ++c) {       // 16 pages at a time
+                uint32_t s[16];
+                tmem_ld16(tD + (j & 1) * 256 + c * 16, s);
                 tc_wait_ld(s);
-                const int j = j0 + half * 64 + c * 32;      // page of the first column
-                if (j >= page1) continue;
-                if (j < begin || __any_sync(0xffffffffu, j + 32 > stop)) {
+                const int k = page0 + first_page(j) + half * 64 + c * 16;      // page of the first column
+                if (k >= page1) continue;
+                if (k < begin || __any_sync(0xffffffffu, k + 16 > stop)) {
 #pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        if (j + i < begin || j + i >= stop) s[i] = 0xff800000u;   // -inf
+                    for (int i = 0; i < 16; ++i)
+                        if (k + i < begin || k + i >= stop) s[i] = 0xff800000u;   // -inf
                 }
-                if (pass == 0) {
+                if (first_pass) {
                     if (gp == 0) {
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) mx[i] = fmaxf(mx[i], __uint_as_float(s[i]));
+                        for (int i = 0; i < 16; ++i) mx[(c & 1) * 16 + i] = fmaxf(mx[(c & 1) * 16 + i], __uint_as_float(s[i]));
                     } else if (my_row < n) {
-                        float4* const to = reinterpret_cast<float4*>(my_maxima + (j - page0) / gp);
+                        float4* const to = reinterpret_cast<float4*>(my_maxima + (k - page0) / gp);
                         auto at = [&](int i) { return __uint_as_float(s[i]); };
                         auto two = [&](int i) { return fmaxf(at(2 * i), at(2 * i + 1)); };
                         auto four = [&](int i) { return fmax3(at(4 * i), at(4 * i + 1), fmaxf(at(4 * i + 2), at(4 * i + 3))); };
                         if (gp == 4) {
-#pragma unroll
-                            for (int i = 0; i < 2; ++i) to[i] = make_float4(four(4 * i), four(4 * i + 1), four(4 * i + 2), four(4 * i + 3));
+                            to[0] = make_float4(four(0), four(1), four(2), four(3));
                         } else if (gp == 2) {
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) to[i] = make_float4(two(4 * i), two(4 * i + 1), two(4 * i + 2), two(4 * i + 3));
+                            for (int i = 0; i < 2; ++i) to[i] = make_float4(two(4 * i), two(4 * i + 1), two(4 * i + 2), two(4 * i + 3));
                         } else {
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) to[i] = make_float4(at(4 * i), at(4 * i + 1), at(4 * i + 2), at(4 * i + 3));
+                            for (int i = 0; i < 4; ++i) to[i] = make_float4(at(4 * i), at(4 * i + 1), at(4 * i + 2), at(4 * i + 3));
                         }
                     }
-                } else if (to_next - found <= p.cap - 32) {      // (room for them all: no check at each)
+                } else if (put_at - list0 + 16 * sizeof(SelectCandidate) <= list_room) {      // (room for them all: no check at each)
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) {
+                    for (int i = 0; i < 16; ++i) {
                         const float y = __uint_as_float(s[i]);
-                        if (y >= floor) *to_next++ = SelectCandidate{y, j + i};
+                        if (y >= floor) put(y, k + i);
                     }
                 } else {
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) {
+                    for (int i = 0; i < 16; ++i) {
                         const float y = __uint_as_float(s[i]);
                         if (y >= floor) {
-                            if (to_next - found < p.cap) *to_next++ = SelectCandidate{y, j + i};
+                            if (put_at - list0 < list_room) put(y, k + i);
                             else ++m;
                         }
                     }
                 }
                 __syncwarp();
             }
-            tc_fence_before();
         }
-        if (!alive || pass == 1) continue;
+        tc_fence_before();
+        if (!borders) continue;
         // ---- the borders ----
-        const uint32_t warp_top = __reduce_max_sync(0xffffffffu, top);
-        if (lane == 0) atomicMax(s_max, warp_top);
+        share_bounds();
+        // the left halves' maxima go to the threads of the right halves for odd rows, the others the other way: a thread a token with all 64.  The place is that
+        // of the operand that is not in use (the step under way uses the other one).
+        float* const swap = reinterpret_cast<float*>(sB + (j & 1) * kSelectB);      // [32][256]: 32 KB
+        const bool mine = gp == 0 && (my_row & 1) == half;
+        if (gp == 0 && !mine) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) swap[i * kSelectItem + my_row] = mx[i];
+        }
         __syncthreads();
         if (gp == 0) {
-            // a thread a token (each twice): its 64 maxima, half of them from the other half's thread through the operand's place
-            float* const other = reinterpret_cast<float*>(sB) + my_row;       // [32][128], twice: 32 KB
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-                if (half == 1) other[i * kSelectTile] = mx[i];
-            __syncthreads();
-            float f = INFINITY;          // (lists without choice, or bounds that say nothing: no candidates)
-            if (half == 0) {
-                const float bound = my_row < n ? select_bound(s_a[my_row], *s_max) : 0.f;
+            if (mine && my_row < n) {
+                const float bound = bound_of(my_row);
+                float f = INFINITY;          // (lists without choice, or bounds that say nothing: no candidates)
                 if (stop > begin && bound > 0.f && bound < INFINITY) {
                     f = -3.4e38f;
                     if (stop - begin > p.cap) {
                         float mo[32];
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) mo[i] = other[i * kSelectTile];
-                        uint32_t t = 0;      // the need-th largest of them, 16 bits of it
-#pragma unroll 1
-                        for (int b = 31; b >= 16; --b) {
-                            const float c = key_value(t | (1u << b));
-                            int k = 0;
+                        for (int i = 0; i < 32; ++i) mo[i] = swap[i * kSelectItem + my_row];
+                        // a value that at least `need` of them reach, and not many more: the span of the 64 halved eight times
+                        float least = fminf(mx[0], mo[0]), most = fmaxf(mx[0], mo[0]);
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) k += (mx[i] >= c) + (mo[i] >= c);
-                            if (k >= need) t |= 1u << b;
+                        for (int i = 1; i < 32; ++i) {
+                            least = fminf(least, fminf(mx[i], mo[i]));
+                            most = fmax3(most, mx[i], mo[i]);
                         }
-                        f = fmaxf(f, key_value(t) - 2.f * bound);
+                        least = fmaxf(least, f);          // (groups of no pages)
+#pragma unroll 1
+                        for (int b = 0; b < 8; ++b) {
+                            const float c = 0.5f * least + 0.5f * most;
+                            int k[4] = {};
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) k[i & 3] += (mx[i] >= c) + (mo[i] >= c);
+                            if (k[0] + k[1] + k[2] + k[3] >= need) least = c; else most = c;
+                        }
+                        f = fmaxf(f, least - 2.f * bound);
                     }
                 }
-                if (my_row < n) s_floor[my_row] = f;
+                s_floor[my_row] = f;
             }
         } else {
             const int lead_group = (begin - page0) / gp;
             for (int t = warp; t < n; t += kSelectThreads / 32) {
                 const int stop_t = end_of(t);
                 float f = INFINITY;
-                const float bound = select_bound(s_a[t], *s_max);
+                const float bound = bound_of(t);
                 if (stop_t > begin && bound > 0.f && bound < INFINITY) {
                     f = -3.4e38f;
                     if (stop_t - begin > p.cap) {
-                        const float* const mxs = p.maxima + (static_cast<long long>(item) * kSelectTile + t) * row_groups + lead_group;
+                        const float* const mxs = p.maxima + (static_cast<long long>(item) * kSelectItem + t) * row_groups + lead_group;
                         f = fmaxf(f, border_of((stop_t - page0 + gp - 1) / gp - lead_group, need, [&](int i) { return mxs[i]; }) - 2.f * bound);
                     }
                 }
@@ -520,20 +673,19 @@ __global__ void __launch_bounds__(kSelectThreads, 2) block_filter_kernel(const S
             }
         }
         __syncthreads();
+        fetch(j + 2);
         if (my_row < n) floor = s_floor[my_row];
     }
-    const uint32_t warp_top = __reduce_max_sync(0xffffffffu, top);
-    if (lane == 0) atomicMax(s_max, warp_top);
-    if (bad) *s_badp = 1;
+    if (!filter) share_bounds();
     if (*s_abort != 0)
         for (int i = 0; i < 64; ++i) __nanosleep(1000);  // let MMAs in flight drain
     __syncthreads();
     if (my_row < n) {
-        p.counts[list_of(my_row) * 2 + half] = static_cast<int>(to_next - found) + m;
-        if (half == 0) p.bounds[list_of(my_row)] = select_bound(s_a[my_row], *s_max);
+        p.counts[list_of(my_row) * 2 + half] = static_cast<int>((put_at - list0) / sizeof(SelectCandidate)) + m;
+        if (half == 0) p.bounds[list_of(my_row)] = bound_of(my_row);
     }
     if (tid == 0) p.bad[item] = *s_abort != 0 ? 3 /* VPP_DEV_TIMEOUT */ : *s_badp ? 2 /* VPP_DEV_BAD_BLOCK */ : 0;
-    if (warp == 0) tmem_dealloc(tmem, 128);
+    __syncthreads();                      // (tensor memory goes back)
 }
 
 // ---- the border -----------------------------------------------------------------------------------------------------------------
@@ -551,7 +703,7 @@ struct PickScratch {
         double all[kPickGather];              // (pick_thorough)
     };
     int32_t page[kPickGather];
-    int32_t close[kPickClose];                // (entries of page / score)
+    int32_t close[kPickClose], close_page[kPickClose];      // the near ones: entries of page / score, their pages
 };
 constexpr int kPickSmem = static_cast<int>(sizeof(PickScratch)) * (kPickThreads / 32);
 
@@ -564,20 +716,21 @@ struct PickRow {
     int group, num_blocks;
 };
 
-// Scores in 64 bits of n pages -- pages[index[c]], or first + c -- by a warp.  NaN counts as -inf.  (out of line, arguments by value: rare, and
+// Scores in 64 bits of n pages -- pages[c], or first + c -- by a warp.  NaN counts as -inf.  (out of line, arguments by value: rare, and
 // the common path keeps its registers)
-__device__ __noinline__ void exact_scores(PickRow w, const int32_t* pages, const int32_t* index, int first, int n, double* out) {
+__device__ __noinline__ void exact_scores(PickRow w, const int32_t* pages, int first, int n, double* out) {
     const int lane = threadIdx.x & 31;
     double ask[4] = {};
+#pragma unroll 4
     for (int h = 0; h < w.group; ++h) {
-        const uint2 x = *reinterpret_cast<const uint2*>(w.q + h * 256 + lane * 8);
+        const uint2 x = __ldg(reinterpret_cast<const uint2*>(w.q + h * 256 + lane * 8));
         ask[0] += static_cast<double>(bf16_lo(x.x));
         ask[1] += static_cast<double>(bf16_hi(x.x));
         ask[2] += static_cast<double>(bf16_lo(x.y));
         ask[3] += static_cast<double>(bf16_hi(x.y));
     }
     for (int c = 0; c < n; ++c) {
-        const int e = __ldg(w.table + (pages ? pages[index[c]] : first + c));
+        const int e = __ldg(w.table + (pages ? pages[c] : first + c));
         double d = -INFINITY;
         if (e >= 0 && e < w.num_blocks) {        // (an entry out of range is reported already)
             const uint2 x = __ldg(reinterpret_cast<const uint2*>(w.means + e * w.mean_stride + lane * 8));
@@ -625,26 +778,25 @@ __device__ __forceinline__ bool pick_settle(PickScratch& s, const PickRow& w, in
         sure += __popc(__ballot_sync(0xffffffffu, in));
         const uint32_t b = __ballot_sync(0xffffffffu, near);
         const int at = near_n + __popc(b & ((1u << lane) - 1));
-        if (near && at < kPickClose) s.close[at] = i;
+        if (near && at < kPickClose) {
+            s.close[at] = i;
+            s.close_page[at] = s.page[i];
+        }
         near_n += __popc(b);
     }
     const int left = need - sure;         // to be taken of the near ones: 1 .. near_n
     if (left != near_n) {
         if (near_n > kPickClose) return false;
         __syncwarp();
-        exact_scores(w, s.page, s.close, 0, near_n, s.exact);
+        exact_scores(w, s.close_page, 0, near_n, s.exact);
         // losers among the near ones get a page of -1
-        int lost = 0;
         for (int c = lane; c < near_n; c += 32) {
             const double d = s.exact[c];
-            const int page = s.page[s.close[c]];
+            const int page = s.close_page[c];
             int before = 0;
-            for (int j = 0; j < near_n; ++j) before += s.exact[j] > d || (s.exact[j] == d && s.page[s.close[j]] < page);
-            if (before >= left) lost |= 1 << (c >> 5);
+            for (int j = 0; j < near_n; ++j) before += s.exact[j] > d || (s.exact[j] == d && s.close_page[j] < page);
+            if (before >= left) s.page[s.close[c]] = -1;
         }
-        __syncwarp();                     // (all have read the pages)
-        for (int c = lane; c < near_n; c += 32)
-            if ((lost >> (c >> 5)) & 1) s.page[s.close[c]] = -1;
     }
     __syncwarp();
     int kept = 0;
@@ -667,7 +819,7 @@ __device__ __noinline__ void pick_thorough(PickScratch& s, PickRow w, int begin,
     int best = 0;
     for (int j0 = begin; j0 < end; j0 += kPickClose) {
         const int n = min(kPickClose, end - j0), m = best + n;
-        exact_scores(w, nullptr, nullptr, j0, n, s.all + best);
+        exact_scores(w, nullptr, j0, n, s.all + best);
         for (int c = lane; c < n; c += 32) s.page[best + c] = j0 + c;
         __syncwarp();
         // ranks: better scores, then lower pages (the best so far are lower pages than the new ones, and in order of their pages)
@@ -700,8 +852,67 @@ __device__ __noinline__ void pick_thorough(PickScratch& s, PickRow w, int begin,
     }
 }
 
+// The same for the common case, two ascending lists of at most 32 candidates each, a lane a candidate of either, and the pages go straight to `out`, ascending.
+__device__ __forceinline__ void pick_two(PickScratch& s, const PickRow& w, SelectCandidate x, int an, SelectCandidate y, int bn, int need, float delta,
+                                         int32_t* out) {
+    const int lane = threadIdx.x & 31;
+    const uint32_t below = (1u << lane) - 1;
+    if (lane >= an) x = SelectCandidate{-INFINITY, INT32_MAX};
+    if (lane >= bn) y = SelectCandidate{-INFINITY, INT32_MAX};
+    const uint32_t kx = lane < an ? order_key(x.score) : 0, ky = lane < bn ? order_key(y.score) : 0;
+    uint32_t border = 0;
+    for (int bit = 31; bit >= 0; --bit) {
+        const uint32_t c = border | (1u << bit);
+        const int all = __popc(__ballot_sync(0xffffffffu, kx >= c)) + __popc(__ballot_sync(0xffffffffu, ky >= c));
+        if (all >= need) border = c;
+        if (all == need) break;
+    }
+    border = __reduce_min_sync(0xffffffffu, min(kx >= border ? kx : 0xffffffffu, ky >= border ? ky : 0xffffffffu));
+    const float v = key_value(border), hi = v + 2.f * delta, lo = v - 2.f * delta;
+    bool take_x = x.score > hi, take_y = y.score > hi;
+    const bool near_x = !take_x && x.score >= lo, near_y = !take_y && y.score >= lo;
+    const uint32_t nx = __ballot_sync(0xffffffffu, near_x), ny = __ballot_sync(0xffffffffu, near_y);
+    const int left = need - __popc(__ballot_sync(0xffffffffu, take_x)) - __popc(__ballot_sync(0xffffffffu, take_y)), near_n = __popc(nx) + __popc(ny);
+    if (left == near_n) {
+        take_x |= near_x;
+        take_y |= near_y;
+    } else {
+        const int at_x = __popc(nx & below), at_y = __popc(nx) + __popc(ny & below);
+        if (near_x) s.close_page[at_x] = x.page;
+        if (near_y) s.close_page[at_y] = y.page;
+        __syncwarp();
+        exact_scores(w, s.close_page, 0, near_n, s.exact);
+        auto wins = [&](int at, int page) {
+            const double d = s.exact[at];
+            int before = 0;
+            for (int j = 0; j < near_n; ++j) before += s.exact[j] > d || (s.exact[j] == d && s.close_page[j] < page);
+            return before < left;
+        };
+        if (near_x) take_x = wins(at_x, x.page);
+        if (near_y) take_y = wins(at_y, y.page);
+        __syncwarp();
+    }
+    const uint32_t tx = __ballot_sync(0xffffffffu, take_x), ty = __ballot_sync(0xffffffffu, take_y);
+    // how many of the other list lie before a page
+    int in_b = 0, in_a = 0;
+#pragma unroll
+    for (int step = 16; step > 0; step >>= 1) {
+        const int pb = __shfl_sync(0xffffffffu, y.page, in_b + step - 1), pa = __shfl_sync(0xffffffffu, x.page, in_a + step - 1);
+        if (pb < x.page) in_b += step;
+        if (pa < y.page) in_a += step;
+    }
+    {   // (the last of 32)
+        const int pb = __shfl_sync(0xffffffffu, y.page, in_b), pa = __shfl_sync(0xffffffffu, x.page, in_a);
+        if (pb < x.page) ++in_b;
+        if (pa < y.page) ++in_a;
+    }
+    auto first = [](int n) { return n >= 32 ? 0xffffffffu : (1u << n) - 1; };
+    if (take_x) out[__popc(tx & below) + __popc(ty & first(in_b))] = x.page;
+    if (take_y) out[__popc(ty & below) + __popc(tx & first(in_a))] = y.page;
+}
+
 // The first work_blocks blocks pick; the block after them, if there is one, writes the status.
-__global__ void __launch_bounds__(kPickThreads, 4) block_pick_kernel(const SelectParams p, const int work_blocks) {
+__global__ void __launch_bounds__(kPickThreads, 3) block_pick_kernel(const SelectParams p, const int work_blocks) {
     extern __shared__ __align__(16) uint8_t pick_smem[];
     PickScratch* const scratch = reinterpret_cast<PickScratch*>(pick_smem);
     int32_t* const cu = reinterpret_cast<int32_t*>(pick_smem + kPickSmem);
@@ -726,7 +937,27 @@ __global__ void __launch_bounds__(kPickThreads, 4) block_pick_kernel(const Selec
     const int G = p.num_q_heads / p.num_kv_heads, need = p.topk - p.num_first - p.num_last;
     PickScratch& s = scratch[warp];
     const int rows = (p.row1 - p.row0) * p.num_kv_heads, step = work_blocks * (kPickThreads / 32);      // (rows of a slab: far below 2^31)
+    // What the common case reads of a row -- one run: its bound, two counts, and the first 32 of both lists, whatever the counts -- is requested a row ahead.
+    struct Ahead {
+        float delta;
+        int2 count;
+        SelectCandidate x, y;
+    };
+    auto request = [&](int i) {
+        Ahead a{};
+        if (p.runs == 1 && i < rows) {
+            const SelectCandidate* const from = p.found + 2ll * i * p.cap + lane;
+            a.delta = p.bounds[i];
+            a.count = *reinterpret_cast<const int2*>(p.counts + 2ll * i);
+            a.x = from[0];
+            a.y = from[p.cap];
+        }
+        return a;
+    };
+    Ahead next = request(blockIdx.x * (kPickThreads / 32) + warp);
     for (int i = blockIdx.x * (kPickThreads / 32) + warp; i < rows; i += step) {
+        const Ahead now = next;
+        next = request(i + step);
         const int t0 = i / p.num_kv_heads, t = p.row0 + t0, g = i - t0 * p.num_kv_heads;
         const int r = request_of(cu, p.num_reqs, t);
         const int own = (p.prefix_len[r] + (t - cu[r])) >> p.block_shift;
@@ -735,11 +966,18 @@ __global__ void __launch_bounds__(kPickThreads, 4) block_pick_kernel(const Selec
             for (int k = lane; k < p.topk; k += 32) out[k] = k <= own ? k : -1;
             continue;
         }
+        const PickRow w{p.q + (static_cast<long long>(t) * p.num_q_heads + g * G) * 256, p.block_table + static_cast<long long>(r) * p.max_blocks_per_req,
+                        p.means + g * 256, static_cast<long long>(p.num_kv_heads) * 256, G, p.num_blocks};
         // (own + 1 > topk >= first + last: the two ends do not meet, and there are more candidates than needed)
         const int end = select_end(p, own), run0 = p.num_first / p.run_pages, runs = (end + p.run_pages - 1) / p.run_pages;
         for (int k = lane; k < p.topk; k += 32)
             if (k < p.num_first || k >= p.num_first + need) out[k] = k < p.num_first ? k : own + 1 - (p.topk - k);
         if (need == 0) continue;
+        if (p.runs == 1 && now.delta > 0.f && now.delta < INFINITY && now.count.x <= 32 && now.count.y <= 32) {
+            pick_two(s, w, now.x, now.count.x, now.y, now.count.y, need, now.delta, out + p.num_first);
+            __syncwarp();
+            continue;
+        }
         float delta = 0.f;
         bool odd = false;
         for (int k = run0 + lane; k < runs; k += 32) {
@@ -754,8 +992,6 @@ __global__ void __launch_bounds__(kPickThreads, 4) block_pick_kernel(const Selec
             for (int k = lane; k < need; k += 32) out[p.num_first + k] = p.num_first + k;
             continue;
         }
-        const PickRow w{p.q + (static_cast<long long>(t) * p.num_q_heads + g * G) * 256, p.block_table + static_cast<long long>(r) * p.max_blocks_per_req,
-                        p.means + g * 256, static_cast<long long>(p.num_kv_heads) * 256, G, p.num_blocks};
         // the runs' candidates, one behind the other
         int m = 0;
         for (int k = 2 * run0; k < 2 * runs && !odd; ++k) {

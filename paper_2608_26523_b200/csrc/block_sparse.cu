@@ -89,7 +89,7 @@ struct SelectPlan {
     int slab;                   // tokens of a slab
     int run_pages, runs;        // pages of an item, items along a row
     int group_pages, cap;
-    int items;                  // most items of a slab
+    int many_items, few_items;  // most items of a slab: of up to 256 tokens; a request each
     size_t found, counts, bounds, maxima, bad, total;
 };
 
@@ -106,19 +106,22 @@ vpp_status select_plan(const vpp_block_select_args* a, SelectPlan* s) {
     if (a->num_first < 0 || a->num_last < 1 || a->num_first > a->topk || a->num_last > a->topk - a->num_first)
         return fail(VPP_ERR_INVALID_ARG, "need num_first >= 0, num_last >= 1 and num_first + num_last <= topk");
     const long long T = a->total_q > 0 ? a->total_q : 1, H = a->num_kv_heads, N = vpp::kSelectTile;
-    const long long steps = (a->max_seq_len / a->block_size + N) / N;       // of 128 pages along a row
+    const long long I = vpp::kSelectItem, steps = (a->max_seq_len / a->block_size + N) / N;       // of 128 pages along a row
     const int need = a->topk - a->num_first - a->num_last;
     // A border that is the need-th largest of the maxima of groups lets through about need (1 + need * group / (2 * pages)) pages.  Rows of few pages
     // list them all, others have pages enough for twice as many groups as are needed.
     // (Up to 32 are needed: 64 groups, kept in registers.)
     s->group_pages = need <= 32 ? 0 : need <= 64 ? 4 : need <= 128 ? 2 : 1;
     s->cap = need <= 128 ? 128 : 256;
-    auto tiles_of = [&](long long rows) {
-        const long long tiles = (rows + N - 1) / N + a->num_reqs;
-        return tiles < rows ? tiles : rows;           // (every tile has a token)
+    // Launches of no more tokens than requests, or of a few tokens: decode rows alone.
+    const bool few_only = T <= a->num_reqs || T <= vpp::kSelectFew;
+    auto many_of = [&](long long rows) {
+        const long long tiles = (rows + I - 1) / I + a->num_reqs;
+        return few_only ? 0 : tiles < rows ? tiles : rows;           // (every tile has a token)
     };
-    // runs of pages: one where the tiles fill the SMs twice, else as many as do (each lists its own best)
-    long long runs = 2ll * sm_count_or_default() / (tiles_of(T) * H);
+    const long long few = few_only || a->num_reqs > 1 ? a->num_reqs : 0;
+    // runs of pages: one where the items fill the SMs, else as many as do (each lists its own best)
+    long long runs = few_only ? 2ll * sm_count_or_default() / (few * H + 1) : sm_count_or_default() / (((T + I - 1) / I) * H);
     if (runs > 4) runs = 4;
     if (runs > steps / 2) runs = steps / 2;
     const long long least = (steps * N + vpp::kSelectMaxRun - 1) / vpp::kSelectMaxRun;
@@ -127,22 +130,23 @@ vpp_status select_plan(const vpp_block_select_args* a, SelectPlan* s) {
     s->run_pages = static_cast<int>((steps + runs - 1) / runs * N);
     s->runs = static_cast<int>((steps * N + s->run_pages - 1) / s->run_pages);
     const long long list = s->runs * (2ll * s->cap * static_cast<long long>(sizeof(vpp::SelectCandidate)) + 12);     // bytes of a row
-    const long long item = s->group_pages > 0 ? N * (s->run_pages / s->group_pages) * 4 : 0;                                                  // of an item
-    long long slab = vpp::kSelectSlabBytes / (H * (list + item * s->runs / N));
-    slab = slab / N * N;                              // (whole tiles of a long chunk)
-    if (slab < N) slab = N;
+    const long long item = s->group_pages > 0 ? I * (s->run_pages / s->group_pages) * 4 : 0;                        // of an item
+    long long slab = vpp::kSelectSlabBytes / (H * (list + item * s->runs / I));
+    slab = slab / I * I;                              // (whole items of a long chunk)
+    if (slab < I) slab = I;
     if (slab > T) slab = T;
     s->slab = static_cast<int>(slab);
-    const long long items = tiles_of(slab) * H * s->runs;
-    if (items > INT32_MAX) return fail(VPP_ERR_UNSUPPORTED, "too many requests times heads");
-    s->items = static_cast<int>(items);
+    const long long many = many_of(slab) * H * s->runs, few_items = few * H * s->runs;
+    if (many + few_items > INT32_MAX) return fail(VPP_ERR_UNSUPPORTED, "too many requests times heads");
+    s->many_items = static_cast<int>(many);
+    s->few_items = static_cast<int>(few_items);
     const size_t rows = static_cast<size_t>(slab) * H * s->runs;
     s->found = 0;
     s->counts = align_up(rows * 2 * s->cap * sizeof(vpp::SelectCandidate), 256);
     s->bounds = align_up(s->counts + rows * 2 * sizeof(int32_t), 256);
     s->maxima = align_up(s->bounds + rows * sizeof(float), 256);
-    s->bad = align_up(s->maxima + static_cast<size_t>(items) * item, 256);
-    s->total = align_up(s->bad + static_cast<size_t>(items) * sizeof(int32_t), 256);
+    s->bad = align_up(s->maxima + static_cast<size_t>(many) * item, 256);
+    s->total = align_up(s->bad + static_cast<size_t>(many + few_items) * sizeof(int32_t), 256);
     return VPP_OK;
 }
 
@@ -399,18 +403,27 @@ vpp_status vpp_block_select(const vpp_block_select_args* a, vpp_stream_t stream_
     p.bounds = reinterpret_cast<float*>(ws + s.bounds);
     p.maxima = reinterpret_cast<float*>(ws + s.maxima);
     p.bad = reinterpret_cast<int32_t*>(ws + s.bad);
-    p.items = s.items;
+    p.many_items = s.many_items;
+    p.items = s.many_items + s.few_items;
     p.indices = a->indices;
     p.status = a->status;
     const size_t lens = sizeof(int32_t) * (static_cast<size_t>(a->num_reqs) + 1);
-    const size_t smem_scores = vpp::kSelectSmem + 2 * lens, smem_pick = vpp::kPickSmem + lens;
-    cudaError_t ce = cudaFuncSetAttribute(vpp::block_filter_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem_scores));
+    const size_t smem_many = vpp::kSelectSmem + 4 * static_cast<size_t>(s.run_pages) + 2 * lens, smem_pick = vpp::kPickSmem + lens;
+    const size_t smem_few = 4 * static_cast<size_t>(vpp::kSelectFew) * s.run_pages + lens;
+    cudaError_t ce = cudaSuccess;
+    if (s.many_items > 0) {
+        if (smem_many > 232448) return fail(VPP_ERR_UNSUPPORTED, "too many requests (%d) for chunks of this context length", a->num_reqs);
+        ce = cudaFuncSetAttribute(vpp::block_filter_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem_many));
+    }
+    if (ce == cudaSuccess && s.few_items > 0) ce = cudaFuncSetAttribute(vpp::block_few_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem_few));
     if (ce == cudaSuccess) ce = cudaFuncSetAttribute(vpp::block_pick_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem_pick));
     if (ce != cudaSuccess) return fail(VPP_ERR_CUDA, "page selection attributes: %s", cudaGetErrorString(ce));
     for (int64_t row0 = 0; row0 < a->total_q; row0 += s.slab) {
         p.row0 = static_cast<int32_t>(row0);
         p.row1 = static_cast<int32_t>(row0 + s.slab < a->total_q ? row0 + s.slab : a->total_q);
-        ce = launch(vpp::block_filter_kernel, static_cast<unsigned>(s.items), vpp::kSelectThreads, smem_scores, stream, p);
+        if (s.many_items > 0) ce = launch(vpp::block_filter_kernel, static_cast<unsigned>(s.many_items), vpp::kSelectThreads + 128, smem_many, stream, p);
+        if (ce == cudaSuccess && s.few_items > 0)
+            ce = launch(vpp::block_few_kernel, static_cast<unsigned>(s.few_items), vpp::kFewThreads, smem_few, stream, p, s.many_items == 0 ? 1 : 0);
         if (ce != cudaSuccess) return fail(VPP_ERR_CUDA, "page scores launch: %s", cudaGetErrorString(ce));
         const long long rows = static_cast<long long>(p.row1 - p.row0) * a->num_kv_heads, warps = vpp::kPickThreads / 32;
         long long blocks = (rows + warps - 1) / warps;
