@@ -18,10 +18,12 @@
 //    8192 tokens of 64 heads are 21 us; the products twice 4).  (All scores written down once, 4.6 KB a token and kv-head, and picked
 //    from there: 8192 tokens of 64/4 heads with 1152 pages 420 us.  Blocks of 128 tokens and eight warps, two an SM, that do one thing after the other: 6500 clk
 //    a step of the two, 115 of 195 us.)
-//  * block_few_kernel: requests of up to kSelectFew tokens -- decode rows -- with the dot products in registers, half a warp a page, and the scores in
+//  * block_few_kernel: requests of up to kSelectFew tokens -- decode rows -- multiplied by warps from the registers that the loads fill, the scores in
 //    shared memory: there reading the means is all.
 //  * block_pick_kernel: a warp a (token, kv-head) ranks the candidates and settles the border.
 #pragma once
+#include <cuda_bf16.h>
+
 #include <cstdint>
 
 #include "lengths.cuh"
@@ -37,10 +39,10 @@ constexpr int kSelectThreads = 512;           // of block_filter_kernel, beside 
 constexpr int kSelectRegsLow = 24, kSelectRegsHigh = 112;
 static_assert(4 * kSelectRegsHigh + kSelectRegsLow <= 5 * 96, "register budget");
 constexpr int kSelectFew = 4;
-constexpr int kFewThreads = 256;
+constexpr int kFewThreads = 512;
 constexpr int kSelectSlabBytes = 128 << 20;
 constexpr int kSelectMaxTopk = 256;
-constexpr int kSelectMaxRun = 4096;           // pages of an item: scores of kSelectFew tokens, or their places, are kept in shared memory
+constexpr int kSelectMaxRun = 4096;           // pages of an item: their scores, or their places, are kept in shared memory
 constexpr int kSelectA = 2 * 2 * kSelectTile * 128;   // an accumulator's operand: two bf16 parts of 128 x 128, two 64-feature slabs each
 constexpr int kSelectB = 2 * kSelectTile * 128;
 constexpr int kSelectSmem = 2 * kSelectA + 2 * kSelectB + 1024 /* alignment */ + 4096 /* barriers, borders */;      // and the pages, the lengths
@@ -79,45 +81,38 @@ struct SelectParams {
 // Candidates of a token whose own page is `own`: pages [num_first, end).
 __device__ __forceinline__ int select_end(const SelectParams& p, int own) { return own + 1 - p.num_last; }
 
-// |x| as ordered bits: NaN above infinity above everything finite
-__device__ __forceinline__ uint32_t abs_max(uint32_t m, uint4 v) {
+// Sum of the squares of a vector's features, as the bits of a float that order as integers: NaN above infinity above everything finite.  (Maxima of |feature| by integer
+// comparisons took 8 of 34 us of 16 decode rows.)
+__device__ __forceinline__ uint64_t square_sums(uint64_t acc, uint4 v) {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        m = max(m, w[e] & 0x7fffu);
-        m = max(m, (w[e] >> 16) & 0x7fffu);
+        const uint64_t x = pack_f32x2(bf16_lo(w[e]), bf16_hi(w[e]));
+        acc = fma_f32x2(x, x, acc);
     }
-    return m;
+    return acc;
 }
-// sum of the squares of a vector's features
-__device__ __forceinline__ float square_sum(uint4 v) {
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-    float a = 0.f, b = 0.f;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        a = fmaf(bf16_lo(w[e]), bf16_lo(w[e]), a);
-        b = fmaf(bf16_hi(w[e]), bf16_hi(w[e]), b);
-    }
+__device__ __forceinline__ float pair_sum(uint64_t v) {
+    float a, b;
+    unpack_f32x2(v, a, b);
     return a + b;
 }
-// What bounds the error of a run's scores: of the means (one pair a block, by atomicMax of their bits: NaN is above infinity above everything finite) the largest |feature|
-// and the largest sum of a page's squares; of a token the sum of its queries' |features| over the group and the sum of squares of the summed query s.
+// The bound on the error of a run's scores.  Of the means: mean_part, the largest sum of squares of a part of a page's features, mean_square, at least the largest of a whole
+// page's (bits).  Of the token: sum_q, the sum of its queries' |features| over the group, square_s, the sum of squares of the summed query s.
 //
-//     |fp32 score - exact score| <= c |s| |mean| + G 2^-23 sum|q| max|mean feature|          (|.|: 2-norms)
+//     |fp32 score - exact score| <= c |s| |mean| + G 2^-23 sum_q max|mean feature|          (|.|: 2-norms)
 //
-// by Cauchy and Schwarz.  c covers forming the product: by the tensor cores 2^-14 (the split leaves 2^-18 of s; 256 products are accumulated with at most 2^-23 of their
-// absolute sum lost each: 2^-15), in registers 2^-19 (8 products and 4 levels of sums of 2^-24).  The second term covers forming s: G - 1 additions of 2^-24 each.
-// Exactly 0 where all products are; infinite or NaN where anything is, or where products could overflow.  (With sum|q| max|mean feature| in place of the norms two thirds of
-// all rows had pages too close to tell, and 8192 tokens of 64/4 heads took 166 us.)
-__device__ __forceinline__ float select_bound(float c, int group, float sum_q, float square_s, uint32_t max_bits, uint32_t square_bits) {
-    const float m = __uint_as_float(max_bits << 16), n2 = __uint_as_float(square_bits);
+// by Cauchy and Schwarz.  c covers forming the product: by the tensor cores 2^-14 (the split leaves 2^-17 of s; 256 products are accumulated with at most 2^-23 of their
+// absolute sum lost each: 2^-15), in registers 2^-19 (16 products and 4 levels of sums of 2^-24).  The second term covers forming s: G - 1 additions of 2^-24 each.
+// (Squares below 2^-149 vanish: features below 1e-22 are taken as that.)  0 where the queries are; infinite or NaN where anything is, or where products could overflow.
+// (With sum_q max|mean feature| in place of the norms two thirds of all rows had pages too close to tell, and 8192 tokens of 64/4 heads took 166 us.)
+__device__ __forceinline__ float select_bound(float c, int group, float sum_q, float square_s, uint32_t mean_part, float mean_square) {
     if (!(sum_q < 1e38f)) return INFINITY;
-    if (sum_q == 0.f && max_bits < 0x7f80u) return 0.f;
-    if (max_bits == 0) return 0.f;
-    const float spread = sum_q * m;
-    // (squares that vanish in 32 bits say nothing)
-    const float product = square_s > 1e-30f && n2 > 1e-30f ? sqrtf(square_s) * sqrtf(n2) * 1.001f : spread;
-    return c * product + static_cast<float>(group) * 1.1920929e-7f * spread + 1e-35f;
+    const float m = sqrtf(__uint_as_float(mean_part)) * 1.001f + 1e-22f, n = sqrtf(mean_square) * 1.001f + 2e-21f;
+    if (sum_q == 0.f && m < INFINITY) return 0.f;
+    // (the 2-norm of s is no more than sum_q)
+    const float s = square_s > 1e-30f ? sqrtf(square_s) * 1.001f : sum_q;
+    return c * (s * n) + static_cast<float>(group) * 1.1920929e-7f * (sum_q * m) + 1e-35f;
 }
 
 // Unsigned integers in the order of floats; NaN below everything.
@@ -167,148 +162,188 @@ __device__ __forceinline__ int slab_rows(const SelectParams& p, const int32_t* c
     return n > 0 ? n : 0;
 }
 
-// Requests of few tokens (with few_only set, of any number, kSelectFew at a time): a block a (request, kv-head, run of pages).
-__global__ void __launch_bounds__(kFewThreads) block_few_kernel(const SelectParams p, const int few_only) {
-    extern __shared__ float s_score[];                              // [kSelectFew][run_pages], then cu [num_reqs + 1]
-    __shared__ uint32_t s_max, s_square;
-    __shared__ int s_bad;
-    int32_t* const cu = reinterpret_cast<int32_t*>(s_score + kSelectFew * p.run_pages);
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, v = tid & 15;
+// D += A B, 16 x 8 += 16 x 16 times 16 x 8, bf16, by a warp
+__device__ __forceinline__ void mma_16x8(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// Requests of up to `most` tokens: a block a (request, kv-head, run of pages), and `slots` of them for its tokens, one at a time.  Reading the means is all that takes time, if it goes
+// with few instructions: 16 pages a warp and round, multiplied by small matrix instructions straight from the registers that the loads fill (each lane's features are a
+// permutation of the product's inner index that the other operand shares).  The columns of that operand are the two parts of the summed query, and for the absolute
+// products that bound the error -- the same registers without signs -- those of the parts and of sum_h |q_h|.  (Dot products in registers, eight lanes a page: 400 instructions
+// for 16 pages instead of 70; 16 rows of 64/4 heads with 2300 pages took 32 us with the page selection behind it, and take 27.)
+__global__ void __launch_bounds__(kFewThreads) block_few_kernel(const SelectParams p, const int slots, const int most) {
+    extern __shared__ float s_score[];                              // [run_pages], then cu [num_reqs + 1]
+    constexpr int kWarps = kFewThreads / 32;
+    __shared__ __align__(16) __nv_bfloat16 s_ask[3][128];           // the summed query's parts, sum_h |q_h|
+    __shared__ uint32_t s_product, s_forming;                       // largest sums of absolute products (bits)
+    __shared__ float s_largest[kFewThreads], s_floor;
+    __shared__ int s_count[kWarps], s_bad;
+    int32_t* const cu = reinterpret_cast<int32_t*>(s_score + p.run_pages);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, gr = lane >> 2, tq = lane & 3;
     if (tid == 0) s_bad = 0;
     pdl_launch_dependents();
     pdl_wait();
     const bool ok = scan_lengths<kFewThreads>(p.prefix_len, p.chunk_len, p.num_reqs, p.capacity, p.total_q, cu);
     int32_t* const flag = p.bad + p.many_items + blockIdx.x;
-    const int run = blockIdx.x % p.runs, rg = blockIdx.x / p.runs, g = rg % p.num_kv_heads, r = rg / p.num_kv_heads;
+    int id = blockIdx.x;
+    const int run = id % p.runs, g = (id /= p.runs) % p.num_kv_heads, slot = (id /= p.num_kv_heads) % slots, r = id / slots;
     int lo;
     const int rows = ok ? slab_rows(p, cu, r, lo) : 0;
-    if (rows == 0 || (rows > kSelectFew && !few_only)) {
+    if (rows == 0 || rows > most) {
         if (tid == 0) *flag = ok ? 0 : 1 /* VPP_DEV_BAD_LENGTHS */;
         return;
     }
     const int G = p.num_q_heads / p.num_kv_heads, need = p.topk - p.num_first - p.num_last;
     const int32_t* const table = p.block_table + static_cast<long long>(r) * p.max_blocks_per_req;
+    const uint8_t* const means = p.means + g * 256 + tq * 16;
+    const long long mean_stride = static_cast<long long>(p.num_kv_heads) * 256;
     bool bad = false;
-    for (int row = lo; row < lo + rows; row += kSelectFew) {
-        const int n = min(kSelectFew, lo + rows - row), pos0 = p.prefix_len[r] + (row - cu[r]);
-        const int end = select_end(p, (pos0 + n - 1) >> p.block_shift);      // of the last token
-        // a page run that nobody needs: below the first candidate, past the last, or no token has more pages than it may list
-        const int page0 = run * p.run_pages, page1 = min(page0 + p.run_pages, end), begin = max(page0, p.num_first);
-        if (page1 <= begin || ((pos0 + n - 1) >> p.block_shift) + 1 <= p.topk) continue;
-        __syncthreads();                  // (the last round's scores are read)
-        if (tid == 0) s_max = s_square = 0;
-        const uint8_t* const q0 = p.q + (static_cast<long long>(row) * p.num_q_heads + g * G) * 256;
-        float s[kSelectFew][8], a[kSelectFew];
-#pragma unroll
-        for (int t = 0; t < kSelectFew; ++t) {
-            a[t] = 0.f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) s[t][e] = 0.f;
-            if (t < n) {
-                const uint8_t* src = q0 + static_cast<long long>(t) * p.num_q_heads * 256 + v * 16;
-#pragma unroll 8
-                for (int h = 0; h < G; ++h) {
-                    const uint4 x = ld_once(src + h * 256);
-                    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        s[t][2 * e] += bf16_lo(w[e]);
-                        s[t][2 * e + 1] += bf16_hi(w[e]);
-                        a[t] += fabsf(bf16_lo(w[e])) + fabsf(bf16_hi(w[e]));
-                    }
-                }
-            }
-#pragma unroll
-            for (int o = 8; o > 0; o >>= 1) a[t] += __shfl_xor_sync(0xffffffffu, a[t], o);
-        }
-        constexpr int kDeep = 8, kStep = kDeep * (kFewThreads / 16);
-        const int half = tid >> 4;
-        uint32_t top = 0;
-        float square = 0.f;
-        int e[kDeep];
+    for (int row = lo + slot; row < lo + rows; row += slots) {
+        const int own = (p.prefix_len[r] + (row - cu[r])) >> p.block_shift;
+        // a page run that nobody needs: below the first candidate, past the last, or the token has no more pages than it may list
+        const int page0 = run * p.run_pages, page1 = min(page0 + p.run_pages, select_end(p, own)), begin = max(page0, p.num_first);
+        if (page1 <= begin || own + 1 <= p.topk) continue;
+        // rows gr and gr + 8 of a round's 16 pages; -1: counts as 0 (pages that are taken anyway: what theirs hold must not widen the bound)
+        int e[2];
         auto look = [&](int j0) {
 #pragma unroll
-            for (int i = 0; i < kDeep; ++i) {
-                const int j = j0 + i * (kFewThreads / 16) + half;
-                e[i] = j < page1 ? __ldg(table + j) : 0;
+            for (int i = 0; i < 2; ++i) {
+                const int j = j0 + gr + 8 * i;
+                e[i] = j >= begin && j < page1 ? __ldg(table + j) : -1;
+                bad |= j >= begin && j < page1 && (e[i] < 0 || e[i] >= p.num_blocks);
             }
         };
-        look(page0);
-        for (int j0 = page0; j0 < page1; j0 += kStep) {
-            uint4 x[kDeep];
+        uint4 x[2][8];
+        auto fetch = [&](uint4 (&to)[8]) {
 #pragma unroll
-            for (int i = 0; i < kDeep; ++i) {
-                const int j = j0 + i * (kFewThreads / 16) + half;
+            for (int i = 0; i < 2; ++i) {
                 const bool fine = e[i] >= 0 && e[i] < p.num_blocks;
-                bad |= !fine;
-                x[i] = make_uint4(0, 0, 0, 0);        // (pages that are taken anyway count as 0: what theirs hold must not widen the bound)
-                if (j < page1 && j >= begin && fine) x[i] = ld_once(p.means + (static_cast<long long>(e[i]) * p.num_kv_heads + g) * 256 + v * 16);
-            }
-            look(j0 + kStep);
+                const uint8_t* const from = means + (fine ? e[i] : 0) * mean_stride;
 #pragma unroll
-            for (int i = 0; i < kDeep; ++i) {
-                const int j = j0 + i * (kFewThreads / 16) + half;
-                top = abs_max(top, x[i]);
-                float sq = square_sum(x[i]);
-#pragma unroll
-                for (int o = 8; o > 0; o >>= 1) sq += __shfl_xor_sync(0xffffffffu, sq, o);
-                square = sq > square || !(sq == sq) ? sq : square;      // (NaN stays)
-                const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-#pragma unroll
-                for (int t = 0; t < kSelectFew; ++t) {
-                    if (t >= n) break;
-                    float d = 0.f;
-#pragma unroll
-                    for (int f = 0; f < 4; ++f) {
-                        d = fmaf(s[t][2 * f], bf16_lo(w[f]), d);
-                        d = fmaf(s[t][2 * f + 1], bf16_hi(w[f]), d);
-                    }
-#pragma unroll
-                    for (int o = 8; o > 0; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
-                    if (v == 0 && j < page1) s_score[t * p.run_pages + j - page0] = d;
+                for (int v = 0; v < 4; ++v) {
+                    to[4 * i + v] = make_uint4(0, 0, 0, 0);
+                    if (fine) to[4 * i + v] = ld_once(from + v * 64);
                 }
             }
+        };
+        const int first = page0 + warp * 16;
+        constexpr int kStep = kWarps * 16;
+        look(first);
+        fetch(x[0]);
+        look(first + kStep);
+        fetch(x[1]);
+        look(first + 2 * kStep);
+        __syncthreads();                  // (the last token's query, scores and bounds are read)
+        bool some = false;
+        if (tid < 128) {
+            float s = 0.f, a = 0.f;
+            const __nv_bfloat16* const q = reinterpret_cast<const __nv_bfloat16*>(p.q) + (static_cast<long long>(row) * p.num_q_heads + g * G) * 128 + tid;
+#pragma unroll 8
+            for (int h = 0; h < G; ++h) {
+                const float y = __bfloat162float(q[h * 128]);
+                s += y;
+                a += fabsf(y);
+            }
+            const __nv_bfloat16 hi = __float2bfloat16(s);
+            s_ask[0][tid] = hi;
+            s_ask[1][tid] = __float2bfloat16(s - __bfloat162float(hi));
+            s_ask[2][tid] = __float2bfloat16(fmaxf(a, 1e-30f));      // (parts below 2^-126 are cut at 2^-134: less than 2^-23 of that.  NaN and infinity show in the parts)
+            some = a != 0.f;
         }
-        __syncthreads();                  // (s_max is 0)
-        top = __reduce_max_sync(0xffffffffu, top);
-        const uint32_t warp_square = __reduce_max_sync(0xffffffffu, __float_as_uint(square) & 0x7fffffffu);
+        if (tid == 0) s_product = s_forming = 0;
+        const bool zero = !__syncthreads_or(some);
+        // column gr of the operands: vector tq + 4 v of the features, two steps of the product in each
+        uint32_t ask[16];
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            uint4 y = make_uint4(0, 0, 0, 0);
+            if (gr < 3) y = *reinterpret_cast<const uint4*>(&s_ask[gr][(tq + 4 * v) * 8]);
+            ask[4 * v] = y.x;
+            ask[4 * v + 1] = y.y;
+            ask[4 * v + 2] = y.z;
+            ask[4 * v + 3] = y.w;
+        }
+        uint32_t product = 0, forming = 0;
+        auto multiply = [&](const uint4 (&y)[8], int j0) {
+            float d[4] = {}, n[4] = {};
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                const uint4 a = y[v], b = y[4 + v];
+                constexpr uint32_t kAbs = 0x7fff7fffu;
+                mma_16x8(d, a.x, b.x, a.y, b.y, ask[4 * v], ask[4 * v + 1]);
+                mma_16x8(n, a.x & kAbs, b.x & kAbs, a.y & kAbs, b.y & kAbs, ask[4 * v] & kAbs, ask[4 * v + 1] & kAbs);
+                mma_16x8(d, a.z, b.z, a.w, b.w, ask[4 * v + 2], ask[4 * v + 3]);
+                mma_16x8(n, a.z & kAbs, b.z & kAbs, a.w & kAbs, b.w & kAbs, ask[4 * v + 2] & kAbs, ask[4 * v + 3] & kAbs);
+            }
+            if (tq == 0) {                // columns 0 and 1: the parts
+                if (j0 + gr < page1) s_score[j0 + gr - page0] = d[0] + d[1];
+                if (j0 + gr + 8 < page1) s_score[j0 + gr + 8 - page0] = d[2] + d[3];
+                product = max(product, max(__float_as_uint(n[0] + n[1]) & 0x7fffffffu, __float_as_uint(n[2] + n[3]) & 0x7fffffffu));
+            } else if (tq == 1) {         // column 2
+                forming = max(forming, max(__float_as_uint(n[0]) & 0x7fffffffu, __float_as_uint(n[2]) & 0x7fffffffu));
+            }
+        };
+        for (int j0 = first; j0 < page1; j0 += 2 * kStep) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                multiply(x[k], j0 + k * kStep);
+                fetch(x[k]);
+                look(j0 + (k + 3) * kStep);
+            }
+        }
+        product = __reduce_max_sync(0xffffffffu, product);
+        forming = __reduce_max_sync(0xffffffffu, forming);
         if (lane == 0) {
-            atomicMax(&s_max, top);
-            atomicMax(&s_square, warp_square);
+            atomicMax(&s_product, product);
+            atomicMax(&s_forming, forming);
+        }
+        __syncthreads();                  // (the scores are there)
+        // The border: a warp's part of the pages, a maximum a lane; the first warp takes the need-th largest of them all.  (One warp through all pages: 5 us of 2048.)
+        const float* const mine = s_score - page0;
+        const int part = (page1 - begin + 32 * kWarps - 1) / (32 * kWarps) * 32, from = min(page1, begin + warp * part), to = min(page1, from + part);
+        float largest = -INFINITY;
+        for (int j = from + lane; j < to; j += 32) largest = fmaxf(largest, mine[j]);
+        s_largest[tid] = largest;
+        __syncthreads();
+        // as select_bound, from the absolute products themselves: the split leaves 2^-17 of s, 128 products of either part are accumulated, 16 and the sum so far a step, with at most 2^-23
+        // of their absolute sum lost each, together below 2^-15 of it; forming s G - 1 additions of 2^-24 (1.01: sum_h |q_h| is rounded)
+        const float worst = __uint_as_float(s_product) * 3.0517578e-5f + __uint_as_float(s_forming) * (1.01f * 1.1920929e-7f) * G;
+        const float bound = worst < 1e34f ? (zero ? 0.f : worst + 1e-35f) : INFINITY;
+        const long long list = (static_cast<long long>(row - p.row0) * p.num_kv_heads + g) * p.runs + run;
+        const bool any = bound > 0.f && bound < INFINITY;
+        if (warp == 0) {
+            // (more than 512 are never needed, and where there are fewer than are needed, that is that many pages or fewer a lane, all are listed)
+            float f = -INFINITY;
+            if (any && page1 - begin > p.cap) f = border_below<kWarps>(kFewThreads, need, [&](int i) { return s_largest[i]; }) - 2.f * bound;
+            if (lane == 0) s_floor = f;
         }
         __syncthreads();
-        if (warp >= n) continue;
-        float at = 0.f, ss = 0.f;
-#pragma unroll
-        for (int t = 0; t < kSelectFew; ++t)
-            if (warp == t) {
-                at = a[t];
-#pragma unroll
-                for (int k = 0; k < 8; ++k) ss = fmaf(s[t][k], s[t][k], ss);
-            }
-#pragma unroll
-        for (int o = 8; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-        const float bound = select_bound(1.9073486e-6f /* 2^-19 */, G, at, ss, s_max, s_square);
-        const int own = (pos0 + warp) >> p.block_shift, stop = own + 1 <= p.topk ? 0 : min(page1, select_end(p, own));
-        const long long list = (static_cast<long long>(row - p.row0 + warp) * p.num_kv_heads + g) * p.runs + run;
-        const float* const mine = s_score + warp * p.run_pages - page0;
+        const float floor = any ? s_floor : INFINITY;
         int m = 0;
-        if (bound > 0.f && bound < INFINITY && stop > begin) {
-            const float floor = stop - begin <= p.cap ? -INFINITY : border_of(stop - begin, need, [&](int i) { return mine[begin + i]; }) - 2.f * bound;
-            SelectCandidate* const found = p.found + list * 2 * p.cap;
-            for (int j0 = begin; j0 < stop; j0 += 32) {
-                const int j = j0 + lane;
-                const float x = j < stop ? mine[j] : 0.f;
-                const bool take = j < stop && x >= floor;
-                const uint32_t b = __ballot_sync(0xffffffffu, take);
-                const int at_m = m + __popc(b & ((1u << lane) - 1));
-                if (take && at_m < p.cap) found[at_m] = SelectCandidate{x, j};
-                m += __popc(b);
-            }
+        for (int j0 = from; j0 < to; j0 += 32) m += __popc(__ballot_sync(0xffffffffu, j0 + lane < to && mine[j0 + lane] >= floor));
+        if (lane == 0) s_count[warp] = m;
+        __syncthreads();
+        int at = 0, all = 0;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+            if (w < warp) at += s_count[w];
+            all += s_count[w];
         }
-        if (lane == 0) {
+        SelectCandidate* const found = p.found + list * 2 * p.cap;
+        for (int j0 = from; j0 < to; j0 += 32) {
+            const int j = j0 + lane;
+            const float y = j < to ? mine[j] : 0.f;
+            const bool take = j < to && y >= floor;
+            const uint32_t b = __ballot_sync(0xffffffffu, take);
+            const int k = at + __popc(b & ((1u << lane) - 1));
+            if (take && k < p.cap) found[k] = SelectCandidate{y, j};
+            at += __popc(b);
+        }
+        if (tid == 0) {
             p.bounds[list] = bound;
-            p.counts[list * 2] = m;
+            p.counts[list * 2] = all;
             p.counts[list * 2 + 1] = 0;
         }
     }
@@ -484,7 +519,7 @@ __global__ void __launch_bounds__(kSelectThreads + 128, 1) block_filter_kernel(c
     // ============================ the others: operands, scores ============================
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSelectRegsHigh));
     uint32_t top = 0, square = 0;
-    auto bound_of = [&](int t) { return select_bound(6.1035156e-5f /* 2^-14 */, G, s_a[t], s_ss[t], *s_max, *s_square); };
+    auto bound_of = [&](int t) { return select_bound(6.1035156e-5f /* 2^-14 */, G, s_a[t], s_ss[t], *s_max, __uint_as_float(*s_square)); };
     auto share_bounds = [&]() {           // the means' part, before a barrier
         const uint32_t a = __reduce_max_sync(0xffffffffu, top), b = __reduce_max_sync(0xffffffffu, square);
         if (lane == 0) {
@@ -517,8 +552,8 @@ __global__ void __launch_bounds__(kSelectThreads + 128, 1) block_filter_kernel(c
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const uint4 x = *reinterpret_cast<const uint4*>(sB + place_of(j, i));
-                top = abs_max(top, x);
-                float sq = square_sum(x);
+                float sq = pair_sum(square_sums(0, x));
+                top = max(top, __float_as_uint(sq) & 0x7fffffffu);
 #pragma unroll
                 for (int o = 8; o > 0; o >>= 1) sq += __shfl_xor_sync(0xffffffffu, sq, o);
                 square = max(square, __float_as_uint(sq) & 0x7fffffffu);
@@ -994,17 +1029,35 @@ __global__ void __launch_bounds__(kPickThreads, 3) block_pick_kernel(const Selec
         }
         // the runs' candidates, one behind the other
         int m = 0;
-        for (int k = 2 * run0; k < 2 * runs && !odd; ++k) {
-            const int c = p.counts[static_cast<long long>(i) * p.runs * 2 + k];
-            odd = c > p.cap || m + c > kPickGather || !(p.bounds[static_cast<long long>(i) * p.runs + (k >> 1)] > 0.f);      // (a run whose scores are all 0 lists none)
-            if (odd) break;
-            const SelectCandidate* const from = p.found + (static_cast<long long>(i) * p.runs * 2 + k) * p.cap;
-            for (int j = lane; j < c; j += 32) {
-                const SelectCandidate x = from[j];
-                s.score[m + j] = x.score;
-                s.page[m + j] = x.page;
+        for (int k0 = 2 * run0; k0 < 2 * runs && !odd; k0 += 32) {
+            const int k = k0 + lane, c = k < 2 * runs ? p.counts[static_cast<long long>(i) * p.runs * 2 + k] : 0;
+            // (a run whose scores are all 0 lists none)
+            odd = __any_sync(0xffffffffu, c > p.cap || (k < 2 * runs && !(p.bounds[static_cast<long long>(i) * p.runs + (k >> 1)] > 0.f)));
+            for (int l0 = 0; l0 < min(32, 2 * runs - k0) && !odd; l0 += 4) {
+                int count[4], at[4];
+                SelectCandidate x[4];
+#pragma unroll
+                for (int l = 0; l < 4; ++l) {      // (four lists' first 32 under way at a time)
+                    count[l] = __shfl_sync(0xffffffffu, c, l0 + l);
+                    at[l] = m;
+                    m += count[l];
+                    if (lane < count[l]) x[l] = p.found[(static_cast<long long>(i) * p.runs * 2 + k0 + l0 + l) * p.cap + lane];
+                }
+                odd = m > kPickGather;
+                if (odd) break;
+#pragma unroll
+                for (int l = 0; l < 4; ++l) {
+                    if (lane < count[l]) {
+                        s.score[at[l] + lane] = x[l].score;
+                        s.page[at[l] + lane] = x[l].page;
+                    }
+                    for (int j = lane + 32; j < count[l]; j += 32) {
+                        const SelectCandidate y = p.found[(static_cast<long long>(i) * p.runs * 2 + k0 + l0 + l) * p.cap + j];
+                        s.score[at[l] + j] = y.score;
+                        s.page[at[l] + j] = y.page;
+                    }
+                }
             }
-            m += c;
         }
         __syncwarp();
         if (odd || !pick_settle(s, w, m, need, delta)) pick_thorough(s, w, p.num_first, end, need);

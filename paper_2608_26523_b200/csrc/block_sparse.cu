@@ -89,6 +89,7 @@ struct SelectPlan {
     int slab;                   // tokens of a slab
     int run_pages, runs;        // pages of an item, items along a row
     int group_pages, cap;
+    int few_slots;              // items of a request of few tokens
     int many_items, few_items;  // most items of a slab: of up to 256 tokens; a request each
     size_t found, counts, bounds, maxima, bad, total;
 };
@@ -119,11 +120,15 @@ vpp_status select_plan(const vpp_block_select_args* a, SelectPlan* s) {
         const long long tiles = (rows + I - 1) / I + a->num_reqs;
         return few_only ? 0 : tiles < rows ? tiles : rows;           // (every tile has a token)
     };
-    const long long few = few_only || a->num_reqs > 1 ? a->num_reqs : 0;
-    // runs of pages: one where the items fill the SMs, else as many as do (each lists its own best)
-    long long runs = few_only ? 2ll * sm_count_or_default() / (few * H + 1) : sm_count_or_default() / (((T + I - 1) / I) * H);
-    if (runs > 4) runs = 4;
-    if (runs > steps / 2) runs = steps / 2;
+    // (a block a request, or several, for its tokens)
+    s->few_slots = T <= a->num_reqs ? 1 : vpp::kSelectFew;
+    const long long few = few_only || a->num_reqs > 1 ? static_cast<long long>(a->num_reqs) * s->few_slots : 0;
+    // Runs of pages, each of which lists its own best: one where the items fill half of the SMs, else as many as fill them all, of 1024 pages or more (decode rows: those
+    // are read in 5 us) or 256.
+    const long long work = (few_only ? few : many_of(T)) * H, sms = sm_count_or_default();
+    long long runs = work > 0 ? sms / work : 1;
+    const long long shortest = few_only ? 8 : 2;
+    if (runs > steps / shortest) runs = steps / shortest;
     const long long least = (steps * N + vpp::kSelectMaxRun - 1) / vpp::kSelectMaxRun;
     if (runs < least) runs = least;
     if (runs < 1) runs = 1;
@@ -409,7 +414,7 @@ vpp_status vpp_block_select(const vpp_block_select_args* a, vpp_stream_t stream_
     p.status = a->status;
     const size_t lens = sizeof(int32_t) * (static_cast<size_t>(a->num_reqs) + 1);
     const size_t smem_many = vpp::kSelectSmem + 4 * static_cast<size_t>(s.run_pages) + 2 * lens, smem_pick = vpp::kPickSmem + lens;
-    const size_t smem_few = 4 * static_cast<size_t>(vpp::kSelectFew) * s.run_pages + lens;
+    const size_t smem_few = 4 * static_cast<size_t>(s.run_pages) + lens;
     cudaError_t ce = cudaSuccess;
     if (s.many_items > 0) {
         if (smem_many > 232448) return fail(VPP_ERR_UNSUPPORTED, "too many requests (%d) for chunks of this context length", a->num_reqs);
@@ -423,7 +428,8 @@ vpp_status vpp_block_select(const vpp_block_select_args* a, vpp_stream_t stream_
         p.row1 = static_cast<int32_t>(row0 + s.slab < a->total_q ? row0 + s.slab : a->total_q);
         if (s.many_items > 0) ce = launch(vpp::block_filter_kernel, static_cast<unsigned>(s.many_items), vpp::kSelectThreads + 128, smem_many, stream, p);
         if (ce == cudaSuccess && s.few_items > 0)
-            ce = launch(vpp::block_few_kernel, static_cast<unsigned>(s.few_items), vpp::kFewThreads, smem_few, stream, p, s.many_items == 0 ? 1 : 0);
+            ce = launch(vpp::block_few_kernel, static_cast<unsigned>(s.few_items), vpp::kFewThreads, smem_few, stream, p, s.few_slots,
+                        s.many_items == 0 ? INT32_MAX : vpp::kSelectFew);
         if (ce != cudaSuccess) return fail(VPP_ERR_CUDA, "page scores launch: %s", cudaGetErrorString(ce));
         const long long rows = static_cast<long long>(p.row1 - p.row0) * a->num_kv_heads, warps = vpp::kPickThreads / 32;
         long long blocks = (rows + warps - 1) / warps;
