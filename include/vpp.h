@@ -512,7 +512,9 @@ vpp_status vpp_block_means(const vpp_block_means_args *args, vpp_stream_t stream
  *              on the GPU need two.
  * status       optional device int32, zeroed by the call; VPP_DEV_BAD_LENGTHS (nothing is written), VPP_DEV_BAD_BLOCK (a page that is scored has an entry
  *              outside [0, num_blocks): lists undefined, but in range) or VPP_DEV_TIMEOUT.
- * Returns after enqueueing two kernels on `stream`, two more for each further 64 MiB of scores (total_q * num_kv_heads * max_seq_len / block_size * 4 bytes).
+ * Candidates are kept for up to 128 MiB worth of tokens at a time: the workspace stays near that however long the chunk is (and goes above it only with hundreds of
+ * kv-heads, or where max_seq_len has millions of pages; past 4 GiB VPP_ERR_UNSUPPORTED).  Its size depends on topk: a smaller one may need more.
+ * Returns after enqueueing two or three kernels on `stream` for each of those portions of the tokens.
  */
 typedef struct {
     const void *q;

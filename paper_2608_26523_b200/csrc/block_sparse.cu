@@ -146,6 +146,8 @@ vpp_status select_plan(const vpp_block_select_args* a, SelectPlan* s) {
     s->many_items = static_cast<int>(many);
     s->few_items = static_cast<int>(few_items);
     const size_t rows = static_cast<size_t>(slab) * H * s->runs;
+    if (rows > UINT32_MAX / (2 * s->cap * sizeof(vpp::SelectCandidate)))            // (byte offsets of candidates have 32 bits)
+        return fail(VPP_ERR_UNSUPPORTED, "too many kv-heads times pages of max_seq_len");
     s->found = 0;
     s->counts = align_up(rows * 2 * s->cap * sizeof(vpp::SelectCandidate), 256);
     s->bounds = align_up(s->counts + rows * 2 * sizeof(int32_t), 256);

@@ -222,3 +222,20 @@ def test_two_streams_and_a_graph():
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(out, select(q, means, table, prefix, chunk, page, 16, 1, 1))
+
+
+@pytest.mark.parametrize("hkv, topk", [(8, 200), (1, 256), (8, 90)])
+def test_portions_of_a_long_chunk(hkv, topk):
+    """Candidates of all tokens take more than a portion of the workspace; requests begin and end inside one, decode rows among them."""
+    prefix, chunk, page = [60000, 100, 44444, 9000, 30000], [1300, 400, 1, 3, 2300 if hkv == 8 else 9000], 16
+    T = sum(chunk)
+    gen = generator(10)
+    table, pool = paged(gen, prefix, chunk, page)
+    q, means = randn(gen, T, 8, 128), randn(gen, pool, hkv, 128)
+    got = select(q, means, table, prefix, chunk, page, topk, 1, 2).cpu().numpy()
+    cu = np.concatenate([[0], np.cumsum(chunk)])
+    m64, tab = f64(means), table.cpu().numpy()
+    for t in sorted({0, 255, 256, 700, 767, 768, 1023, 1024, 1279, 1280, 1299, 1300, 1535, 1536, 1699, 1700, 1701, 1702, 1703, 1704, 2047, 2048, 2303, 2304, 3000, T - 1}):
+        r = int(np.searchsorted(cu, t, side="right")) - 1
+        row = ref_block_select(f64(q[t:t + 1]), m64, tab[r:r + 1], [prefix[r] + t - int(cu[r])], [1], page, topk, 1, 2)
+        assert (got[t] == row[0]).all(), t
