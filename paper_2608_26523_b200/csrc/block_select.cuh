@@ -81,38 +81,35 @@ struct SelectParams {
 // Candidates of a token whose own page is `own`: pages [num_first, end).
 __device__ __forceinline__ int select_end(const SelectParams& p, int own) { return own + 1 - p.num_last; }
 
-// Sum of the squares of a vector's features, as the bits of a float that order as integers: NaN above infinity above everything finite.  (Maxima of |feature| by integer
-// comparisons took 8 of 34 us of 16 decode rows.)
-__device__ __forceinline__ uint64_t square_sums(uint64_t acc, uint4 v) {
+// Bound on the error of an item's scores, formed by the tensor cores from the two parts of the summed query:
+//
+//     |fp32 score - exact score| <= (2^-14 |s| + G 2^-23 |a|) |mean|          s = sum_h q_h,  a = sum_h |q_h| (features);  |.|: 2-norms
+//
+// by Cauchy and Schwarz.  The split leaves 2^-17 of s; 256 products are accumulated, 16 and the sum so far a step, with at most 2^-23 of their absolute sum lost each: 2^-15.
+// Forming s is G - 1 additions of at most 2^-24 of a feature's a each.  token_weight is what stands before |mean|: 0 where the queries are 0, infinite where anything is or
+// where products could overflow.  (Squares may vanish: below 1e-30 the sum of a is taken, which is no less than either norm.)
+// (With the largest feature of the means and the sum of all |q| in place of the norms two thirds of all rows had pages too close to tell.)
+__device__ __forceinline__ float token_weight(int group, float sum_a, float square_a, float square_s) {
+    if (!(sum_a < 1e38f)) return INFINITY;
+    const float s = square_s > 1e-30f ? sqrtf(square_s) * 1.001f : sum_a, a = square_a > 1e-30f ? sqrtf(square_a) * 1.001f : sum_a;
+    return 6.1035156e-5f * s + static_cast<float>(group) * 1.1920929e-7f * a;
+}
+// square: the largest sum of squares of a page's features as mean_square forms it (bits; NaN above infinity above everything finite).
+__device__ __forceinline__ float select_bound(float weight, uint32_t square) {
+    const float norm = sqrtf(__uint_as_float(square) * 1.02f) * 1.001f + 2e-18f;
+    if (weight == 0.f && norm < INFINITY) return 0.f;
+    return weight * norm + 1e-35f;
+}
+// Sum of squares of 8 features, at least 0.98 of it (four roundings to bf16); features below 1e-19 may be lost.
+__device__ __forceinline__ float mean_square(uint4 v) {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    __nv_bfloat162 acc = __floats2bfloat162_rn(0.f, 0.f);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        const uint64_t x = pack_f32x2(bf16_lo(w[e]), bf16_hi(w[e]));
-        acc = fma_f32x2(x, x, acc);
+        const __nv_bfloat162 x = *reinterpret_cast<const __nv_bfloat162*>(&w[e]);
+        acc = __hfma2(x, x, acc);
     }
-    return acc;
-}
-__device__ __forceinline__ float pair_sum(uint64_t v) {
-    float a, b;
-    unpack_f32x2(v, a, b);
-    return a + b;
-}
-// The bound on the error of a run's scores.  Of the means: mean_part, the largest sum of squares of a part of a page's features, mean_square, at least the largest of a whole
-// page's (bits).  Of the token: sum_q, the sum of its queries' |features| over the group, square_s, the sum of squares of the summed query s.
-//
-//     |fp32 score - exact score| <= c |s| |mean| + G 2^-23 sum_q max|mean feature|          (|.|: 2-norms)
-//
-// by Cauchy and Schwarz.  c covers forming the product: by the tensor cores 2^-14 (the split leaves 2^-17 of s; 256 products are accumulated with at most 2^-23 of their
-// absolute sum lost each: 2^-15), in registers 2^-19 (16 products and 4 levels of sums of 2^-24).  The second term covers forming s: G - 1 additions of 2^-24 each.
-// (Squares below 2^-149 vanish: features below 1e-22 are taken as that.)  0 where the queries are; infinite or NaN where anything is, or where products could overflow.
-// (With sum_q max|mean feature| in place of the norms two thirds of all rows had pages too close to tell, and 8192 tokens of 64/4 heads took 166 us.)
-__device__ __forceinline__ float select_bound(float c, int group, float sum_q, float square_s, uint32_t mean_part, float mean_square) {
-    if (!(sum_q < 1e38f)) return INFINITY;
-    const float m = sqrtf(__uint_as_float(mean_part)) * 1.001f + 1e-22f, n = sqrtf(mean_square) * 1.001f + 2e-21f;
-    if (sum_q == 0.f && m < INFINITY) return 0.f;
-    // (the 2-norm of s is no more than sum_q)
-    const float s = square_s > 1e-30f ? sqrtf(square_s) * 1.001f : sum_q;
-    return c * (s * n) + static_cast<float>(group) * 1.1920929e-7f * (sum_q * m) + 1e-35f;
+    return __low2float(acc) + __high2float(acc);
 }
 
 // Unsigned integers in the order of floats; NaN below everything.
@@ -307,7 +304,7 @@ __global__ void __launch_bounds__(kFewThreads) block_few_kernel(const SelectPara
         for (int j = from + lane; j < to; j += 32) largest = fmaxf(largest, mine[j]);
         s_largest[tid] = largest;
         __syncthreads();
-        // as select_bound, from the absolute products themselves: the split leaves 2^-17 of s, 128 products of either part are accumulated, 16 and the sum so far a step, with at most 2^-23
+        // as token_weight, from the absolute products themselves: the split leaves 2^-17 of s, 128 products of either part are accumulated, 16 and the sum so far a step, with at most 2^-23
         // of their absolute sum lost each, together below 2^-15 of it; forming s G - 1 additions of 2^-24 (1.01: sum_h |q_h| is rounded)
         const float worst = __uint_as_float(s_product) * 3.0517578e-5f + __uint_as_float(s_forming) * (1.01f * 1.1920929e-7f) * G;
         const float bound = worst < 1e34f ? (zero ? 0.f : worst + 1e-35f) : INFINITY;
@@ -362,19 +359,16 @@ __global__ void __launch_bounds__(kSelectThreads + 128, 1) block_filter_kernel(c
     const uint32_t bar = base + 2 * kSelectA + 2 * kSelectB;           // [2] scores of a buffer
     volatile int* const s_abort = reinterpret_cast<volatile int*>(sX + 16);
     volatile uint32_t* const s_tmem = reinterpret_cast<volatile uint32_t*>(sX + 20);
-    uint32_t* const s_max = reinterpret_cast<uint32_t*>(sX + 24);
     int* const s_badp = reinterpret_cast<int*>(sX + 28);
     uint32_t* const s_square = reinterpret_cast<uint32_t*>(sX + 32);
-    float* const s_a = reinterpret_cast<float*>(sX + 64);              // [256] what a bound is made of: sum of |q|
-    float* const s_ss = s_a + kSelectItem;                             // [256] and the summed query's squares
-    float* const s_floor = s_ss + kSelectItem;                         // [256] lowest score of a candidate
+    float* const s_weight = reinterpret_cast<float*>(sX + 64);         // [256] what a token's bound is made of
+    float* const s_floor = s_weight + kSelectItem;                         // [256] lowest score of a candidate
     int32_t* const s_page = reinterpret_cast<int32_t*>(sX + 4096);     // [run_pages] physical page, -1: counts as 0
     int32_t* const cu = s_page + p.run_pages;                          // [num_reqs + 1], then items before request r [num_reqs + 1]
     int32_t* const first_item = cu + p.num_reqs + 1;
 
     if (tid == 0) {
         *s_abort = 0;
-        *s_max = 0;
         *s_square = 0;
         *s_badp = 0;
         mbar_init(bar, 1);
@@ -440,7 +434,7 @@ __global__ void __launch_bounds__(kSelectThreads + 128, 1) block_filter_kernel(c
     if (tid < kSelectThreads) {
         const uint8_t* const q0 = p.q + (static_cast<long long>(row) * p.num_q_heads + g * G) * 256 + v * 16;
         for (int t = tid >> 4; t < n; t += kSelectThreads / 16) {
-            float s[8] = {}, a = 0.f;
+            float s[8] = {}, a[8] = {};
             const uint8_t* const src = q0 + static_cast<long long>(t) * p.num_q_heads * 256;
 #pragma unroll 8
             for (int h = 0; h < G; ++h) {
@@ -450,16 +444,22 @@ __global__ void __launch_bounds__(kSelectThreads + 128, 1) block_filter_kernel(c
                 for (int k = 0; k < 4; ++k) {
                     s[2 * k] += bf16_lo(w[k]);
                     s[2 * k + 1] += bf16_hi(w[k]);
-                    a += fabsf(bf16_lo(w[k])) + fabsf(bf16_hi(w[k]));
+                    a[2 * k] += fabsf(bf16_lo(w[k]));
+                    a[2 * k + 1] += fabsf(bf16_hi(w[k]));
                 }
             }
             const unsigned half_mask = 0xffffu << (lane & 16);        // (the other half's token may not exist)
-            float ss = 0.f;
+            float ss = 0.f, aa = 0.f, sum = 0.f;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) ss = fmaf(s[k], s[k], ss);
+            for (int k = 0; k < 8; ++k) {
+                ss = fmaf(s[k], s[k], ss);
+                aa = fmaf(a[k], a[k], aa);
+                sum += a[k];
+            }
 #pragma unroll
             for (int o = 8; o > 0; o >>= 1) {
-                a += __shfl_xor_sync(half_mask, a, o);
+                sum += __shfl_xor_sync(half_mask, sum, o);
+                aa += __shfl_xor_sync(half_mask, aa, o);
                 ss += __shfl_xor_sync(half_mask, ss, o);
             }
             uint32_t hi[4], rest[4];
@@ -471,10 +471,7 @@ __global__ void __launch_bounds__(kSelectThreads + 128, 1) block_filter_kernel(c
             uint8_t* const to = gen + (t >> 7) * kSelectA + (v >> 3) * (kSelectTile * 128) + (t & 127) * 128 + (((v & 7) ^ (t & 7)) << 4);
             *reinterpret_cast<uint4*>(to) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
             *reinterpret_cast<uint4*>(to + kSelectA / 2) = make_uint4(rest[0], rest[1], rest[2], rest[3]);
-            if (v == 0) {
-                s_a[t] = a;
-                s_ss[t] = ss;
-            }
+            if (v == 0) s_weight[t] = token_weight(G, sum, aa, ss);
         }
     }
     tc_fence_before();
@@ -518,14 +515,11 @@ __global__ void __launch_bounds__(kSelectThreads + 128, 1) block_filter_kernel(c
     }
     // ============================ the others: operands, scores ============================
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSelectRegsHigh));
-    uint32_t top = 0, square = 0;
-    auto bound_of = [&](int t) { return select_bound(6.1035156e-5f /* 2^-14 */, G, s_a[t], s_ss[t], *s_max, __uint_as_float(*s_square)); };
+    uint32_t square = 0;
+    auto bound_of = [&](int t) { return select_bound(s_weight[t], *s_square); };
     auto share_bounds = [&]() {           // the means' part, before a barrier
-        const uint32_t a = __reduce_max_sync(0xffffffffu, top), b = __reduce_max_sync(0xffffffffu, square);
-        if (lane == 0) {
-            atomicMax(s_max, a);
-            atomicMax(s_square, b);
-        }
+        const uint32_t b = __reduce_max_sync(0xffffffffu, square);
+        if (lane == 0) atomicMax(s_square, b);
     };
     // The thread's four vectors of the means of step j, of rows tid / 16 + 32 i, on the way into the operand's place; zeros where there is no page.
     auto place_of = [&](int j, int i) -> uint32_t {
@@ -549,15 +543,16 @@ __global__ void __launch_bounds__(kSelectThreads + 128, 1) block_filter_kernel(c
     auto landed = [&](int j) {            // the thread's own copies of step j are done, and seen by the tensor core after the barrier that follows
         asm volatile("cp.async.wait_all;" ::: "memory");
         if (j < per_pass) {
+            // sums of squares of four rows, 16 lanes each: a lane goes on with two of them, then with one
+            float sq[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint4 x = *reinterpret_cast<const uint4*>(sB + place_of(j, i));
-                float sq = pair_sum(square_sums(0, x));
-                top = max(top, __float_as_uint(sq) & 0x7fffffffu);
-#pragma unroll
-                for (int o = 8; o > 0; o >>= 1) sq += __shfl_xor_sync(0xffffffffu, sq, o);
-                square = max(square, __float_as_uint(sq) & 0x7fffffffu);
-            }
+            for (int i = 0; i < 4; ++i) sq[i] = mean_square(*reinterpret_cast<const uint4*>(sB + place_of(j, i)));
+            const bool up = lane & 8, right = lane & 4;
+            const float a = (up ? sq[2] : sq[0]) + __shfl_xor_sync(0xffffffffu, up ? sq[0] : sq[2], 8), b = (up ? sq[3] : sq[1]) + __shfl_xor_sync(0xffffffffu, up ? sq[1] : sq[3], 8);
+            float c = (right ? b : a) + __shfl_xor_sync(0xffffffffu, right ? a : b, 4);
+            c += __shfl_xor_sync(0xffffffffu, c, 2);
+            c += __shfl_xor_sync(0xffffffffu, c, 1);
+            square = max(square, __float_as_uint(c) & 0x7fffffffu);
         }
         fence_proxy_async_smem();
     };
@@ -569,12 +564,12 @@ __global__ void __launch_bounds__(kSelectThreads + 128, 1) block_filter_kernel(c
     const int gp = p.group_pages, row_groups = gp > 0 ? p.run_pages / gp : 0;
     float* const my_maxima = p.maxima + (static_cast<long long>(item) * kSelectItem + my_row) * row_groups;
     float floor = -3.4e38f;      // (below every score that counts and above the -inf of pages that are no candidates)
-    // (a slab's lists are far below 4 GB: offsets of 32 bits, one instruction to move on)
-    const uint32_t list0 = static_cast<uint32_t>((list_of(my_row) * 2 + half) * p.cap * sizeof(SelectCandidate)), list_room = p.cap * sizeof(SelectCandidate);
-    uint32_t put_at = list0;
+    SelectCandidate* const list0 = p.found + (list_of(my_row) * 2 + half) * p.cap;
+    SelectCandidate* put_at = list0;
+    // (predicated: two of three columns have a row that lists them, and a branch around every store took 20 clk a column instead of XX)
     auto put = [&](float score, int page) {
-        *reinterpret_cast<SelectCandidate*>(reinterpret_cast<uint8_t*>(p.found) + put_at) = SelectCandidate{score, page};
-        put_at += sizeof(SelectCandidate);
+        asm volatile("{\n.reg .pred q;\nsetp.ge.f32 q, %1, %2;\n@q st.global.v2.b32 [%0], {%3, %4};\n@q add.u64 %0, %0, 8;\n}"
+                     : "+l"(put_at) : "f"(score), "f"(floor), "r"(__float_as_uint(score)), "r"(page) : "memory");
     };
     int m = 0;                   // those that found no room
     float mx[32];                // gp == 0: of the pages that are column i of a piece
@@ -597,23 +592,40 @@ __global__ void __launch_bounds__(kSelectThreads + 128, 1) block_filter_kernel(c
         const bool first_pass = filter && j < per_pass;
         tc_fence_after();
         if (alive && tile_lives) {
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {       // 16 pages at a time
-                uint32_t s[16];
-                tmem_ld16(tD + (j & 1) * 256 + c * 16, s);
-                tc_wait_ld(s);
-                const int k = page0 + first_page(j) + half * 64 + c * 16;      // page of the first column
-                if (k >= page1) continue;
+            const int k0 = page0 + first_page(j) + half * 64;
+            uint32_t sc[2][16];                 // 16 pages at a time, k of the first
+            auto mask = [&](uint32_t (&s)[16], int k) {      // those that are no candidates: -inf
                 if (k < begin || __any_sync(0xffffffffu, k + 16 > stop)) {
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
-                        if (k + i < begin || k + i >= stop) s[i] = 0xff800000u;   // -inf
+                        if (k + i < begin || k + i >= stop) s[i] = 0xff800000u;
                 }
-                if (first_pass) {
-                    if (gp == 0) {
+            };
+            if (first_pass && gp == 0) {
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) mx[(c & 1) * 16 + i] = fmaxf(mx[(c & 1) * 16 + i], __uint_as_float(s[i]));
-                    } else if (my_row < n) {
+                for (int c = 0; c < 2; ++c) {
+                    tmem_ld16(tD + (j & 1) * 256 + c * 16, sc[0]);
+                    tmem_ld16(tD + (j & 1) * 256 + (c + 2) * 16, sc[1]);
+                    tc_wait_ld(sc[0]);
+                    tc_wait_ld(sc[1]);
+                    mask(sc[0], k0 + c * 16);
+                    mask(sc[1], k0 + (c + 2) * 16);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) mx[c * 16 + i] = fmax3(mx[c * 16 + i], __uint_as_float(sc[0][i]), __uint_as_float(sc[1][i]));
+                }
+            }
+            if (!(first_pass && gp == 0)) tmem_ld16(tD + (j & 1) * 256, sc[0]);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                if (first_pass && gp == 0) break;
+                uint32_t (&s)[16] = sc[c & 1];
+                tc_wait_ld(s);
+                if (c < 3) tmem_ld16(tD + (j & 1) * 256 + (c + 1) * 16, sc[(c + 1) & 1]);
+                const int k = k0 + c * 16;
+                if (k >= page1) continue;
+                mask(s, k);
+                if (first_pass) {
+                    if (my_row < n) {
                         float4* const to = reinterpret_cast<float4*>(my_maxima + (k - page0) / gp);
                         auto at = [&](int i) { return __uint_as_float(s[i]); };
                         auto two = [&](int i) { return fmaxf(at(2 * i), at(2 * i + 1)); };
@@ -628,20 +640,14 @@ __global__ void __launch_bounds__(kSelectThreads + 128, 1) block_filter_kernel(c
                             for (int i = 0; i < 4; ++i) to[i] = make_float4(at(4 * i), at(4 * i + 1), at(4 * i + 2), at(4 * i + 3));
                         }
                     }
-                } else if (put_at - list0 + 16 * sizeof(SelectCandidate) <= list_room) {      // (room for them all: no check at each)
+                } else if (put_at - list0 + 16 <= p.cap) {      // (room for them all: no check at each)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const float y = __uint_as_float(s[i]);
-                        if (y >= floor) put(y, k + i);
-                    }
+                    for (int i = 0; i < 16; ++i) put(__uint_as_float(s[i]), k + i);
                 } else {
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        const float y = __uint_as_float(s[i]);
-                        if (y >= floor) {
-                            if (put_at - list0 < list_room) put(y, k + i);
-                            else ++m;
-                        }
+                        if (put_at - list0 < p.cap) put(__uint_as_float(s[i]), k + i);
+                        else m += __uint_as_float(s[i]) >= floor;
                     }
                 }
                 __syncwarp();
@@ -651,10 +657,10 @@ __global__ void __launch_bounds__(kSelectThreads + 128, 1) block_filter_kernel(c
         if (!borders) continue;
         // ---- the borders ----
         share_bounds();
-        // the left halves' maxima go to the threads of the right halves for odd rows, the others the other way: a thread a token with all 64.  The place is that
-        // of the operand that is not in use (the step under way uses the other one).
+        // the right halves' maxima go to the threads of the left halves: a thread a token with all 64.  The place is that of the operand that is not in use (the
+        // step under way uses the other one).
         float* const swap = reinterpret_cast<float*>(sB + (j & 1) * kSelectB);      // [32][256]: 32 KB
-        const bool mine = gp == 0 && (my_row & 1) == half;
+        const bool mine = gp == 0 && half == 0;
         if (gp == 0 && !mine) {
 #pragma unroll
             for (int i = 0; i < 32; ++i) swap[i * kSelectItem + my_row] = mx[i];
@@ -716,7 +722,7 @@ __global__ void __launch_bounds__(kSelectThreads + 128, 1) block_filter_kernel(c
         for (int i = 0; i < 64; ++i) __nanosleep(1000);  // let MMAs in flight drain
     __syncthreads();
     if (my_row < n) {
-        p.counts[list_of(my_row) * 2 + half] = static_cast<int>((put_at - list0) / sizeof(SelectCandidate)) + m;
+        p.counts[list_of(my_row) * 2 + half] = static_cast<int>(put_at - list0) + m;
         if (half == 0) p.bounds[list_of(my_row)] = bound_of(my_row);
     }
     if (tid == 0) p.bad[item] = *s_abort != 0 ? 3 /* VPP_DEV_TIMEOUT */ : *s_badp ? 2 /* VPP_DEV_BAD_BLOCK */ : 0;
