@@ -35,8 +35,8 @@ namespace vpp {
 constexpr int kSelectTile = 128;              // tokens of an accumulator, pages of a step
 constexpr int kSelectItem = 256;              // tokens of an item
 constexpr int kSelectThreads = 512;           // of block_filter_kernel, beside the warp that issues and three that make it a group of four
-// Registers a thread after the roles split: the launch gives 96 (five warps a sub-partition), of which the last four warps hand back 72.
-constexpr int kSelectRegsLow = 24, kSelectRegsHigh = 112;
+// Registers a thread after the roles split: the launch gives 96 (five warps a sub-partition), of which the last four warps hand back 32 (72: the thread that issues spills, 132 us instead of 128).
+constexpr int kSelectRegsLow = 64, kSelectRegsHigh = 104;
 static_assert(4 * kSelectRegsHigh + kSelectRegsLow <= 5 * 96, "register budget");
 constexpr int kSelectFew = 4;
 constexpr int kFewThreads = 512;
@@ -83,16 +83,17 @@ __device__ __forceinline__ int select_end(const SelectParams& p, int own) { retu
 
 // Bound on the error of an item's scores, formed by the tensor cores from the two parts of the summed query:
 //
-//     |fp32 score - exact score| <= (2^-14 |s| + G 2^-23 |a|) |mean|          s = sum_h q_h,  a = sum_h |q_h| (features);  |.|: 2-norms
+//     |fp32 score - exact score| <= (13 2^-19 |s| + G 2^-23 |a|) |mean|          s = sum_h q_h,  a = sum_h |q_h| (features);  |.|: 2-norms
 //
-// by Cauchy and Schwarz.  The split leaves 2^-17 of s; 256 products are accumulated, 16 and the sum so far a step, with at most 2^-23 of their absolute sum lost each: 2^-15.
+// by Cauchy and Schwarz.  The split leaves 2^-17 of s.  16 products and the sum so far are added a step, with at most 2^-23 of their absolute sum lost each: 8 steps of the
+// part that is small come first and lose 2^-8 of 2^-16 of |s| |mean|, 8 of the other 17 2^-20.  (4 + 8.5 + 0.04) 2^-19.
 // Forming s is G - 1 additions of at most 2^-24 of a feature's a each.  token_weight is what stands before |mean|: 0 where the queries are 0, infinite where anything is or
 // where products could overflow.  (Squares may vanish: below 1e-30 the sum of a is taken, which is no less than either norm.)
 // (With the largest feature of the means and the sum of all |q| in place of the norms two thirds of all rows had pages too close to tell.)
 __device__ __forceinline__ float token_weight(int group, float sum_a, float square_a, float square_s) {
     if (!(sum_a < 1e38f)) return INFINITY;
     const float s = square_s > 1e-30f ? sqrtf(square_s) * 1.001f : sum_a, a = square_a > 1e-30f ? sqrtf(square_a) * 1.001f : sum_a;
-    return 6.1035156e-5f * s + static_cast<float>(group) * 1.1920929e-7f * a;
+    return 2.4795532e-5f * s + static_cast<float>(group) * 1.1920929e-7f * a;
 }
 // square: the largest sum of squares of a page's features as mean_square forms it (bits; NaN above infinity above everything finite).
 __device__ __forceinline__ float select_bound(float weight, uint32_t square) {
@@ -497,7 +498,7 @@ __global__ void __launch_bounds__(kSelectThreads + 128, 1) block_filter_kernel(c
 #pragma unroll
                     for (int k = 0; k < 16; ++k) {
                         const uint32_t at = (((k >> 2) & 1) * (kSelectTile * 128) + (k & 3) * 32) >> 4;
-                        mma_ss_lhh(tmem + (j & 1) * 256 + t * 128, a0 + (k >> 3) * (kSelectA / 2 >> 4) + at, kHi, b0 + at, kHi, kIdesc, k > 0);
+                        mma_ss_lhh(tmem + (j & 1) * 256 + t * 128, a0 + (1 - (k >> 3)) * (kSelectA / 2 >> 4) + at, kHi, b0 + at, kHi, kIdesc, k > 0);
                     }
                 }
                 tc_commit(bar + 8 * (j & 1));
@@ -762,7 +763,7 @@ struct PickRow {
 __device__ __noinline__ void exact_scores(PickRow w, const int32_t* pages, int first, int n, double* out) {
     const int lane = threadIdx.x & 31;
     double ask[4] = {};
-#pragma unroll 4
+#pragma unroll 8
     for (int h = 0; h < w.group; ++h) {
         const uint2 x = __ldg(reinterpret_cast<const uint2*>(w.q + h * 256 + lane * 8));
         ask[0] += static_cast<double>(bf16_lo(x.x));
