@@ -166,12 +166,13 @@ __device__ __forceinline__ void mma_16x8(float (&d)[4], uint32_t a0, uint32_t a1
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// Requests of up to `most` tokens: a block a (request, kv-head, run of pages), and `slots` of them for its tokens, one at a time.  Reading the means is all that takes time, if it goes
+// Few tokens: a block a (token, kv-head, run of pages); by_token 1: any token of the slab (launches of decode rows: however the tokens lie in the requests), 0: one of
+// kSelectFew places of every request, of which those with more tokens are left to block_filter_kernel.  Reading the means is all that takes time, if it goes
 // with few instructions: 16 pages a warp and round, multiplied by small matrix instructions straight from the registers that the loads fill (each lane's features are a
 // permutation of the product's inner index that the other operand shares).  The columns of that operand are the two parts of the summed query, and for the absolute
 // products that bound the error -- the same registers without signs -- those of the parts and of sum_h |q_h|.  (Dot products in registers, eight lanes a page: 400 instructions
 // for 16 pages instead of 70; 16 rows of 64/4 heads with 2300 pages took 32 us with the page selection behind it, and take 27.)
-__global__ void __launch_bounds__(kFewThreads) block_few_kernel(const SelectParams p, const int slots, const int most) {
+__global__ void __launch_bounds__(kFewThreads) block_few_kernel(const SelectParams p, const int by_token) {
     extern __shared__ float s_score[];                              // [run_pages], then cu [num_reqs + 1]
     constexpr int kWarps = kFewThreads / 32;
     __shared__ __align__(16) __nv_bfloat16 s_ask[3][128];           // the summed query's parts, sum_h |q_h|
@@ -186,10 +187,23 @@ __global__ void __launch_bounds__(kFewThreads) block_few_kernel(const SelectPara
     const bool ok = scan_lengths<kFewThreads>(p.prefix_len, p.chunk_len, p.num_reqs, p.capacity, p.total_q, cu);
     int32_t* const flag = p.bad + p.many_items + blockIdx.x;
     int id = blockIdx.x;
-    const int run = id % p.runs, g = (id /= p.runs) % p.num_kv_heads, slot = (id /= p.num_kv_heads) % slots, r = id / slots;
-    int lo;
-    const int rows = ok ? slab_rows(p, cu, r, lo) : 0;
-    if (rows == 0 || rows > most) {
+    const int run = id % p.runs, g = (id /= p.runs) % p.num_kv_heads;
+    id /= p.num_kv_heads;
+    int r = 0, row = p.row0 + id;
+    bool mine = ok && row < p.row1;
+    if (ok && by_token) {
+        if (mine) r = request_of(cu, p.num_reqs, row);
+    } else if (ok) {
+        int lo;
+        r = id / kSelectFew;
+        const int rows = slab_rows(p, cu, r, lo);
+        row = lo + id % kSelectFew;
+        mine = rows <= kSelectFew && row < lo + rows;
+    }
+    const int own = mine ? (p.prefix_len[r] + (row - cu[r])) >> p.block_shift : 0;
+    // a page run that nobody needs: below the first candidate, past the last, or the token has no more pages than it may list
+    const int page0 = run * p.run_pages, page1 = min(page0 + p.run_pages, select_end(p, own)), begin = max(page0, p.num_first);
+    if (!mine || page1 <= begin || own + 1 <= p.topk) {
         if (tid == 0) *flag = ok ? 0 : 1 /* VPP_DEV_BAD_LENGTHS */;
         return;
     }
@@ -198,152 +212,145 @@ __global__ void __launch_bounds__(kFewThreads) block_few_kernel(const SelectPara
     const uint8_t* const means = p.means + g * 256 + tq * 16;
     const long long mean_stride = static_cast<long long>(p.num_kv_heads) * 256;
     bool bad = false;
-    for (int row = lo + slot; row < lo + rows; row += slots) {
-        const int own = (p.prefix_len[r] + (row - cu[r])) >> p.block_shift;
-        // a page run that nobody needs: below the first candidate, past the last, or the token has no more pages than it may list
-        const int page0 = run * p.run_pages, page1 = min(page0 + p.run_pages, select_end(p, own)), begin = max(page0, p.num_first);
-        if (page1 <= begin || own + 1 <= p.topk) continue;
-        // rows gr and gr + 8 of a round's 16 pages; -1: counts as 0 (pages that are taken anyway: what theirs hold must not widen the bound)
-        int e[2];
-        auto look = [&](int j0) {
+    // rows gr and gr + 8 of a round's 16 pages; -1: counts as 0 (pages that are taken anyway: what theirs hold must not widen the bound)
+    int e[2];
+    auto look = [&](int j0) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int j = j0 + gr + 8 * i;
-                e[i] = j >= begin && j < page1 ? __ldg(table + j) : -1;
-                bad |= j >= begin && j < page1 && (e[i] < 0 || e[i] >= p.num_blocks);
-            }
-        };
-        uint4 x[2][8];
-        auto fetch = [&](uint4 (&to)[8]) {
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const bool fine = e[i] >= 0 && e[i] < p.num_blocks;
-                const uint8_t* const from = means + (fine ? e[i] : 0) * mean_stride;
-#pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                    to[4 * i + v] = make_uint4(0, 0, 0, 0);
-                    if (fine) to[4 * i + v] = ld_once(from + v * 64);
-                }
-            }
-        };
-        const int first = page0 + warp * 16;
-        constexpr int kStep = kWarps * 16;
-        look(first);
-        fetch(x[0]);
-        look(first + kStep);
-        fetch(x[1]);
-        look(first + 2 * kStep);
-        __syncthreads();                  // (the last token's query, scores and bounds are read)
-        bool some = false;
-        if (tid < 128) {
-            float s = 0.f, a = 0.f;
-            const __nv_bfloat16* const q = reinterpret_cast<const __nv_bfloat16*>(p.q) + (static_cast<long long>(row) * p.num_q_heads + g * G) * 128 + tid;
-#pragma unroll 8
-            for (int h = 0; h < G; ++h) {
-                const float y = __bfloat162float(q[h * 128]);
-                s += y;
-                a += fabsf(y);
-            }
-            const __nv_bfloat16 hi = __float2bfloat16(s);
-            s_ask[0][tid] = hi;
-            s_ask[1][tid] = __float2bfloat16(s - __bfloat162float(hi));
-            s_ask[2][tid] = __float2bfloat16(fmaxf(a, 1e-30f));      // (parts below 2^-126 are cut at 2^-134: less than 2^-23 of that.  NaN and infinity show in the parts)
-            some = a != 0.f;
+        for (int i = 0; i < 2; ++i) {
+            const int j = j0 + gr + 8 * i;
+            e[i] = j >= begin && j < page1 ? __ldg(table + j) : -1;
+            bad |= j >= begin && j < page1 && (e[i] < 0 || e[i] >= p.num_blocks);
         }
-        if (tid == 0) s_product = s_forming = 0;
-        const bool zero = !__syncthreads_or(some);
-        // column gr of the operands: vector tq + 4 v of the features, two steps of the product in each
-        uint32_t ask[16];
+    };
+    uint4 x[2][8];
+    auto fetch = [&](uint4 (&to)[8]) {
 #pragma unroll
-        for (int v = 0; v < 4; ++v) {
-            uint4 y = make_uint4(0, 0, 0, 0);
-            if (gr < 3) y = *reinterpret_cast<const uint4*>(&s_ask[gr][(tq + 4 * v) * 8]);
-            ask[4 * v] = y.x;
-            ask[4 * v + 1] = y.y;
-            ask[4 * v + 2] = y.z;
-            ask[4 * v + 3] = y.w;
-        }
-        uint32_t product = 0, forming = 0;
-        auto multiply = [&](const uint4 (&y)[8], int j0) {
-            float d[4] = {}, n[4] = {};
+        for (int i = 0; i < 2; ++i) {
+            const bool fine = e[i] >= 0 && e[i] < p.num_blocks;
+            const uint8_t* const from = means + (fine ? e[i] : 0) * mean_stride;
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
-                const uint4 a = y[v], b = y[4 + v];
-                constexpr uint32_t kAbs = 0x7fff7fffu;
-                mma_16x8(d, a.x, b.x, a.y, b.y, ask[4 * v], ask[4 * v + 1]);
-                mma_16x8(n, a.x & kAbs, b.x & kAbs, a.y & kAbs, b.y & kAbs, ask[4 * v] & kAbs, ask[4 * v + 1] & kAbs);
-                mma_16x8(d, a.z, b.z, a.w, b.w, ask[4 * v + 2], ask[4 * v + 3]);
-                mma_16x8(n, a.z & kAbs, b.z & kAbs, a.w & kAbs, b.w & kAbs, ask[4 * v + 2] & kAbs, ask[4 * v + 3] & kAbs);
+                to[4 * i + v] = make_uint4(0, 0, 0, 0);
+                if (fine) to[4 * i + v] = ld_once(from + v * 64);
             }
-            if (tq == 0) {                // columns 0 and 1: the parts
-                if (j0 + gr < page1) s_score[j0 + gr - page0] = d[0] + d[1];
-                if (j0 + gr + 8 < page1) s_score[j0 + gr + 8 - page0] = d[2] + d[3];
-                product = max(product, max(__float_as_uint(n[0] + n[1]) & 0x7fffffffu, __float_as_uint(n[2] + n[3]) & 0x7fffffffu));
-            } else if (tq == 1) {         // column 2
-                forming = max(forming, max(__float_as_uint(n[0]) & 0x7fffffffu, __float_as_uint(n[2]) & 0x7fffffffu));
-            }
-        };
-        for (int j0 = first; j0 < page1; j0 += 2 * kStep) {
+        }
+    };
+    const int first = page0 + warp * 16;
+    constexpr int kStep = kWarps * 16;
+    look(first);
+    fetch(x[0]);
+    look(first + kStep);
+    fetch(x[1]);
+    look(first + 2 * kStep);
+    bool some = false;
+    if (tid < 128) {
+        float s = 0.f, a = 0.f;
+        const __nv_bfloat16* const q = reinterpret_cast<const __nv_bfloat16*>(p.q) + (static_cast<long long>(row) * p.num_q_heads + g * G) * 128 + tid;
+#pragma unroll 8
+        for (int h = 0; h < G; ++h) {
+            const float y = __bfloat162float(q[h * 128]);
+            s += y;
+            a += fabsf(y);
+        }
+        const __nv_bfloat16 hi = __float2bfloat16(s);
+        s_ask[0][tid] = hi;
+        s_ask[1][tid] = __float2bfloat16(s - __bfloat162float(hi));
+        s_ask[2][tid] = __float2bfloat16(fmaxf(a, 1e-30f));      // (parts below 2^-126 are cut at 2^-134: less than 2^-23 of that.  NaN and infinity show in the parts)
+        some = a != 0.f;
+    }
+    if (tid == 0) s_product = s_forming = 0;
+    const bool zero = !__syncthreads_or(some);
+    // column gr of the operands: vector tq + 4 v of the features, two steps of the product in each
+    uint32_t ask[16];
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                multiply(x[k], j0 + k * kStep);
-                fetch(x[k]);
-                look(j0 + (k + 3) * kStep);
-            }
-        }
-        product = __reduce_max_sync(0xffffffffu, product);
-        forming = __reduce_max_sync(0xffffffffu, forming);
-        if (lane == 0) {
-            atomicMax(&s_product, product);
-            atomicMax(&s_forming, forming);
-        }
-        __syncthreads();                  // (the scores are there)
-        // The border: a warp's part of the pages, a maximum a lane; the first warp takes the need-th largest of them all.  (One warp through all pages: 5 us of 2048.)
-        const float* const mine = s_score - page0;
-        const int part = (page1 - begin + 32 * kWarps - 1) / (32 * kWarps) * 32, from = min(page1, begin + warp * part), to = min(page1, from + part);
-        float largest = -INFINITY;
-        for (int j = from + lane; j < to; j += 32) largest = fmaxf(largest, mine[j]);
-        s_largest[tid] = largest;
-        __syncthreads();
-        // as token_weight, from the absolute products themselves: the split leaves 2^-17 of s, 128 products of either part are accumulated, 16 and the sum so far a step, with at most 2^-23
-        // of their absolute sum lost each, together below 2^-15 of it; forming s G - 1 additions of 2^-24 (1.01: sum_h |q_h| is rounded)
-        const float worst = __uint_as_float(s_product) * 3.0517578e-5f + __uint_as_float(s_forming) * (1.01f * 1.1920929e-7f) * G;
-        const float bound = worst < 1e34f ? (zero ? 0.f : worst + 1e-35f) : INFINITY;
-        const long long list = (static_cast<long long>(row - p.row0) * p.num_kv_heads + g) * p.runs + run;
-        const bool any = bound > 0.f && bound < INFINITY;
-        if (warp == 0) {
-            // (more than 512 are never needed, and where there are fewer than are needed, that is that many pages or fewer a lane, all are listed)
-            float f = -INFINITY;
-            if (any && page1 - begin > p.cap) f = border_below<kWarps>(kFewThreads, need, [&](int i) { return s_largest[i]; }) - 2.f * bound;
-            if (lane == 0) s_floor = f;
-        }
-        __syncthreads();
-        const float floor = any ? s_floor : INFINITY;
-        int m = 0;
-        for (int j0 = from; j0 < to; j0 += 32) m += __popc(__ballot_sync(0xffffffffu, j0 + lane < to && mine[j0 + lane] >= floor));
-        if (lane == 0) s_count[warp] = m;
-        __syncthreads();
-        int at = 0, all = 0;
+    for (int v = 0; v < 4; ++v) {
+        uint4 y = make_uint4(0, 0, 0, 0);
+        if (gr < 3) y = *reinterpret_cast<const uint4*>(&s_ask[gr][(tq + 4 * v) * 8]);
+        ask[4 * v] = y.x;
+        ask[4 * v + 1] = y.y;
+        ask[4 * v + 2] = y.z;
+        ask[4 * v + 3] = y.w;
+    }
+    uint32_t product = 0, forming = 0;
+    auto multiply = [&](const uint4 (&y)[8], int j0) {
+        float d[4] = {}, n[4] = {};
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
-            if (w < warp) at += s_count[w];
-            all += s_count[w];
+        for (int v = 0; v < 4; ++v) {
+            const uint4 a = y[v], b = y[4 + v];
+            constexpr uint32_t kAbs = 0x7fff7fffu;
+            mma_16x8(d, a.x, b.x, a.y, b.y, ask[4 * v], ask[4 * v + 1]);
+            mma_16x8(n, a.x & kAbs, b.x & kAbs, a.y & kAbs, b.y & kAbs, ask[4 * v] & kAbs, ask[4 * v + 1] & kAbs);
+            mma_16x8(d, a.z, b.z, a.w, b.w, ask[4 * v + 2], ask[4 * v + 3]);
+            mma_16x8(n, a.z & kAbs, b.z & kAbs, a.w & kAbs, b.w & kAbs, ask[4 * v + 2] & kAbs, ask[4 * v + 3] & kAbs);
         }
-        SelectCandidate* const found = p.found + list * 2 * p.cap;
-        for (int j0 = from; j0 < to; j0 += 32) {
-            const int j = j0 + lane;
-            const float y = j < to ? mine[j] : 0.f;
-            const bool take = j < to && y >= floor;
-            const uint32_t b = __ballot_sync(0xffffffffu, take);
-            const int k = at + __popc(b & ((1u << lane) - 1));
-            if (take && k < p.cap) found[k] = SelectCandidate{y, j};
-            at += __popc(b);
+        if (tq == 0) {                // columns 0 and 1: the parts
+            if (j0 + gr < page1) s_score[j0 + gr - page0] = d[0] + d[1];
+            if (j0 + gr + 8 < page1) s_score[j0 + gr + 8 - page0] = d[2] + d[3];
+            product = max(product, max(__float_as_uint(n[0] + n[1]) & 0x7fffffffu, __float_as_uint(n[2] + n[3]) & 0x7fffffffu));
+        } else if (tq == 1) {         // column 2
+            forming = max(forming, max(__float_as_uint(n[0]) & 0x7fffffffu, __float_as_uint(n[2]) & 0x7fffffffu));
         }
-        if (tid == 0) {
-            p.bounds[list] = bound;
-            p.counts[list * 2] = all;
-            p.counts[list * 2 + 1] = 0;
+    };
+    for (int j0 = first; j0 < page1; j0 += 2 * kStep) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            multiply(x[k], j0 + k * kStep);
+            fetch(x[k]);
+            look(j0 + (k + 3) * kStep);
         }
+    }
+    product = __reduce_max_sync(0xffffffffu, product);
+    forming = __reduce_max_sync(0xffffffffu, forming);
+    if (lane == 0) {
+        atomicMax(&s_product, product);
+        atomicMax(&s_forming, forming);
+    }
+    __syncthreads();                  // (the scores are there)
+    // The border: a warp's part of the pages, a maximum a lane; the first warp takes the need-th largest of them all.  (One warp through all pages: 5 us of 2048.)
+    const float* const scores = s_score - page0;
+    const int part = (page1 - begin + 32 * kWarps - 1) / (32 * kWarps) * 32, from = min(page1, begin + warp * part), to = min(page1, from + part);
+    float largest = -INFINITY;
+    for (int j = from + lane; j < to; j += 32) largest = fmaxf(largest, scores[j]);
+    s_largest[tid] = largest;
+    __syncthreads();
+    // as token_weight, from the absolute products themselves: the split leaves 2^-17 of s, 128 products of either part are accumulated, 16 and the sum so far a step, with at most 2^-23
+    // of their absolute sum lost each, together below 2^-15 of it; forming s G - 1 additions of 2^-24 (1.01: sum_h |q_h| is rounded)
+    const float worst = __uint_as_float(s_product) * 3.0517578e-5f + __uint_as_float(s_forming) * (1.01f * 1.1920929e-7f) * G;
+    const float bound = worst < 1e34f ? (zero ? 0.f : worst + 1e-35f) : INFINITY;
+    const long long list = (static_cast<long long>(row - p.row0) * p.num_kv_heads + g) * p.runs + run;
+    const bool any = bound > 0.f && bound < INFINITY;
+    if (warp == 0) {
+        // (more than 512 are never needed, and where there are fewer than are needed, that is that many pages or fewer a lane, all are listed)
+        float f = -INFINITY;
+        if (any && page1 - begin > p.cap) f = border_below<kWarps>(kFewThreads, need, [&](int i) { return s_largest[i]; }) - 2.f * bound;
+        if (lane == 0) s_floor = f;
+    }
+    __syncthreads();
+    const float floor = any ? s_floor : INFINITY;
+    int m = 0;
+    for (int j0 = from; j0 < to; j0 += 32) m += __popc(__ballot_sync(0xffffffffu, j0 + lane < to && scores[j0 + lane] >= floor));
+    if (lane == 0) s_count[warp] = m;
+    __syncthreads();
+    int at = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+        if (w < warp) at += s_count[w];
+        all += s_count[w];
+    }
+    SelectCandidate* const found = p.found + list * 2 * p.cap;
+    for (int j0 = from; j0 < to; j0 += 32) {
+        const int j = j0 + lane;
+        const float y = j < to ? scores[j] : 0.f;
+        const bool take = j < to && y >= floor;
+        const uint32_t b = __ballot_sync(0xffffffffu, take);
+        const int k = at + __popc(b & ((1u << lane) - 1));
+        if (take && k < p.cap) found[k] = SelectCandidate{y, j};
+        at += __popc(b);
+    }
+    if (tid == 0) {
+        p.bounds[list] = bound;
+        p.counts[list * 2] = all;
+        p.counts[list * 2 + 1] = 0;
     }
     if (bad) s_bad = 1;
     __syncthreads();

@@ -89,8 +89,7 @@ struct SelectPlan {
     int slab;                   // tokens of a slab
     int run_pages, runs;        // pages of an item, items along a row
     int group_pages, cap;
-    int few_slots;              // items of a request of few tokens
-    int many_items, few_items;  // most items of a slab: of up to 256 tokens; a request each
+    int many_items, few_items;  // most items of a slab: of up to 256 tokens; of one
     size_t found, counts, bounds, maxima, bad, total;
 };
 
@@ -114,15 +113,13 @@ vpp_status select_plan(const vpp_block_select_args* a, SelectPlan* s) {
     // (Up to 32 are needed: 64 groups, kept in registers.)
     s->group_pages = need <= 32 ? 0 : need <= 64 ? 4 : need <= 128 ? 2 : 1;
     s->cap = need <= 128 ? 128 : 256;
-    // Launches of no more tokens than requests, or of a few tokens: decode rows alone.
+    // Launches of no more tokens than requests, or of a few tokens: decode rows alone, an item a token.
     const bool few_only = T <= a->num_reqs || T <= vpp::kSelectFew;
     auto many_of = [&](long long rows) {
         const long long tiles = (rows + I - 1) / I + a->num_reqs;
         return few_only ? 0 : tiles < rows ? tiles : rows;           // (every tile has a token)
     };
-    // (a block a request, or several, for its tokens)
-    s->few_slots = T <= a->num_reqs ? 1 : vpp::kSelectFew;
-    const long long few = few_only || a->num_reqs > 1 ? static_cast<long long>(a->num_reqs) * s->few_slots : 0;
+    const long long few = few_only ? T : a->num_reqs > 1 ? static_cast<long long>(a->num_reqs) * vpp::kSelectFew : 0;
     // Runs of pages, each of which lists its own best: one where the items fill half of the SMs, else as many as fill them all, of 1024 pages or more (decode rows: those
     // are read in 5 us) or 256.
     const long long work = (few_only ? few : many_of(T)) * H, sms = sm_count_or_default();
@@ -141,7 +138,7 @@ vpp_status select_plan(const vpp_block_select_args* a, SelectPlan* s) {
     if (slab < I) slab = I;
     if (slab > T) slab = T;
     s->slab = static_cast<int>(slab);
-    const long long many = many_of(slab) * H * s->runs, few_items = few * H * s->runs;
+    const long long many = many_of(slab) * H * s->runs, few_items = (few_only ? slab : few) * H * s->runs;
     if (many + few_items > INT32_MAX) return fail(VPP_ERR_UNSUPPORTED, "too many requests times heads");
     s->many_items = static_cast<int>(many);
     s->few_items = static_cast<int>(few_items);
@@ -430,8 +427,7 @@ vpp_status vpp_block_select(const vpp_block_select_args* a, vpp_stream_t stream_
         p.row1 = static_cast<int32_t>(row0 + s.slab < a->total_q ? row0 + s.slab : a->total_q);
         if (s.many_items > 0) ce = launch(vpp::block_filter_kernel, static_cast<unsigned>(s.many_items), vpp::kSelectThreads + 128, smem_many, stream, p);
         if (ce == cudaSuccess && s.few_items > 0)
-            ce = launch(vpp::block_few_kernel, static_cast<unsigned>(s.few_items), vpp::kFewThreads, smem_few, stream, p, s.few_slots,
-                        s.many_items == 0 ? INT32_MAX : vpp::kSelectFew);
+            ce = launch(vpp::block_few_kernel, static_cast<unsigned>(s.few_items), vpp::kFewThreads, smem_few, stream, p, s.many_items == 0 ? 1 : 0);
         if (ce != cudaSuccess) return fail(VPP_ERR_CUDA, "page scores launch: %s", cudaGetErrorString(ce));
         const long long rows = static_cast<long long>(p.row1 - p.row0) * a->num_kv_heads, warps = vpp::kPickThreads / 32;
         long long blocks = (rows + warps - 1) / warps;

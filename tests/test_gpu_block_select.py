@@ -239,3 +239,14 @@ def test_portions_of_a_long_chunk(hkv, topk):
         r = int(np.searchsorted(cu, t, side="right")) - 1
         row = ref_block_select(f64(q[t:t + 1]), m64, tab[r:r + 1], [prefix[r] + t - int(cu[r])], [1], page, topk, 1, 2)
         assert (got[t] == row[0]).all(), t
+
+
+def test_no_more_tokens_than_requests_but_a_request_with_most_of_them():
+    """Launches with places for requests that are not there: no request has a token but one, two or three."""
+    page, n = 16, 260
+    for at in ({17: 200}, {0: 100, 259: 1}, {3: 2, 4: 5, 258: 90}):
+        prefix = [(37 * i) % 900 + 600 for i in range(n)]
+        chunk = [at.get(i, 0) for i in range(n)]
+        gen = generator(11)
+        table, pool = paged(gen, prefix, chunk, page)
+        check(randn(gen, sum(chunk), 8, 128), randn(gen, pool, 2, 128), table, prefix, chunk, page, 12, 1, 2)
