@@ -909,8 +909,11 @@ __device__ __forceinline__ void pick_two(PickScratch& s, const PickRow& w, Selec
     if (lane >= an) x = SelectCandidate{-INFINITY, INT32_MAX};
     if (lane >= bn) y = SelectCandidate{-INFINITY, INT32_MAX};
     const uint32_t kx = lane < an ? order_key(x.score) : 0, ky = lane < bn ? order_key(y.score) : 0;
-    uint32_t border = 0;
-    for (int bit = 31; bit >= 0; --bit) {
+    // (from the highest bit in which they differ: candidates are of one size)
+    const uint32_t most = __reduce_max_sync(0xffffffffu, max(kx, ky)), least = __reduce_min_sync(0xffffffffu, min(lane < an ? kx : most, lane < bn ? ky : most));
+    int bit = 31 - __clz(most ^ least);
+    uint32_t border = bit < 0 ? most : most & ~((2u << bit) - 1);
+    for (; bit >= 0; --bit) {
         const uint32_t c = border | (1u << bit);
         const int all = __popc(__ballot_sync(0xffffffffu, kx >= c)) + __popc(__ballot_sync(0xffffffffu, ky >= c));
         if (all >= need) border = c;

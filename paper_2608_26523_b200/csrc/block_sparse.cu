@@ -431,7 +431,7 @@ vpp_status vpp_block_select(const vpp_block_select_args* a, vpp_stream_t stream_
         if (ce != cudaSuccess) return fail(VPP_ERR_CUDA, "page scores launch: %s", cudaGetErrorString(ce));
         const long long rows = static_cast<long long>(p.row1 - p.row0) * a->num_kv_heads, warps = vpp::kPickThreads / 32;
         long long blocks = (rows + warps - 1) / warps;
-        const long long cap = 8ll * sm_count_or_default();
+        const long long cap = 3ll * sm_count_or_default();          // (those that fit at a time; 8: 128 instead of 125 us of 8192 tokens, the last wave half empty)
         if (blocks > cap) blocks = cap;
         const int work_blocks = static_cast<int>(blocks);
         ce = launch(vpp::block_pick_kernel, static_cast<unsigned>(work_blocks + (a->status ? 1 : 0)), vpp::kPickThreads, smem_pick, stream, p, work_blocks);
