@@ -9,18 +9,19 @@
 // the border are closer than the bound allows to tell, theirs are formed again in 64 bits (products of bf16 are exact there).
 //
 // Kernels of a slab of tokens (one slab unless their candidates take more than kSelectSlabBytes):
-//  * block_filter_kernel: an item is (up to 256 tokens of one request, kv-head, a run of pages), a block of 16 warps and one that issues the MMAs.  The group's
-//    queries are summed first, in 32 bits, and the sum split in two bf16 (hi + rest: 16 bits of it), so that the tensor cores do 2 / group
+//  * block_filter_kernel: an item is (up to 256 tokens of one request, kv-head, a run of pages), a block of 16 warps and four that issue the MMAs.  The group's
+//    queries are summed first, in 32 bits, and the sum split in two bf16 (hi + rest), so that the tensor cores do 2 / group
 //    of the work of all q-heads; scores of 128 tokens x 128 pages are one accumulator, and an item has two of those a step, with two buffers: the next step's
 //    products run under this one's scores.  They are formed twice: the first time the maxima of groups
 //    of pages are kept, whose need-th largest bounds a token's border from below; the second time what is not below that by more than the error
-//    bound -- a few more pages than needed -- is written down, a thread a token and half of the pages.  Reading q bounds it (134 MB of
-//    8192 tokens of 64 heads are 21 us; the products twice 4).  (All scores written down once, 4.6 KB a token and kv-head, and picked
-//    from there: 8192 tokens of 64/4 heads with 1152 pages 420 us.  Blocks of 128 tokens and eight warps, two an SM, that do one thing after the other: 6500 clk
-//    a step of the two, 115 of 195 us.)
-//  * block_few_kernel: requests of up to kSelectFew tokens -- decode rows -- multiplied by warps from the registers that the loads fill, the scores in
+//    bound -- a few more pages than needed -- is written down, a thread a token and half of the pages.
+//  * block_few_kernel: tokens of requests of up to kSelectFew -- decode rows -- multiplied by warps from the registers that the loads fill, the scores in
 //    shared memory: there reading the means is all.
 //  * block_pick_kernel: a warp a (token, kv-head) ranks the candidates and settles the border.
+// 8192 tokens of 64/4 heads, 1152 pages, lists of 32: 122 us, of which the filter takes 88: 26 reading 134 MB of q (21 at the copy rate), then 18 steps of 2.4 (maxima)
+// and 4.4 thousand clk (lists), where the products take 2.05; its issue slots bound it, the lists' stores most.  One row of twenty has pages too close for 32 bits (8 us).
+// Before: all scores written down once, 4.6 KB a token and kv-head, and picked from there, 420 us; items of 128 tokens, eight warps that do one thing after the
+// other, two an SM, 195; items of 224 tokens, 148 of them, 130; means fetched and bounded by the four other warps alone, 3900 clk a step for 64 copies.
 #pragma once
 #include <cuda_bf16.h>
 
@@ -574,7 +575,7 @@ __global__ void __launch_bounds__(kSelectThreads + 128, 1) block_filter_kernel(c
     float floor = -3.4e38f;      // (below every score that counts and above the -inf of pages that are no candidates)
     SelectCandidate* const list0 = p.found + (list_of(my_row) * 2 + half) * p.cap;
     SelectCandidate* put_at = list0;
-    // (predicated: two of three columns have a row that lists them, and a branch around every store took 20 clk a column instead of XX)
+    // (predicated: two of three columns have a row that lists them, and a branch around every store took 5100 clk a step of 64 instead of 4400)
     auto put = [&](float score, int page) {
         asm volatile("{\n.reg .pred q;\nsetp.ge.f32 q, %1, %2;\n@q st.global.v2.b32 [%0], {%3, %4};\n@q add.u64 %0, %0, 8;\n}"
                      : "+l"(put_at) : "f"(score), "f"(floor), "r"(__float_as_uint(score)), "r"(page) : "memory");

@@ -116,7 +116,7 @@ vpp_status select_plan(const vpp_block_select_args* a, SelectPlan* s) {
     // Launches of no more tokens than requests, or of a few tokens: decode rows alone, an item a token.
     const bool few_only = T <= a->num_reqs || T <= vpp::kSelectFew;
     auto many_of = [&](long long rows) {
-        const long long tiles = (rows + I - 1) / I + a->num_reqs;
+        const long long tiles = (rows + a->num_reqs * (I - 1)) / I;      // (every request rounds up)
         return few_only ? 0 : tiles < rows ? tiles : rows;           // (every tile has a token)
     };
     const long long few = few_only ? T : a->num_reqs > 1 ? static_cast<long long>(a->num_reqs) * vpp::kSelectFew : 0;
