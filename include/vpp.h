@@ -557,7 +557,7 @@ vpp_status vpp_block_select(const vpp_block_select_args *args, vpp_stream_t stre
  * mask: a page with infinite or NaN VALUES can give NaN to the neighbours (up to 127 tokens away) of the tokens that list it, as a masked key can in
  * vpp_chunk_attn_fwd; infinite or NaN keys of a page touch the tokens that list it only.
  * Cost: keys in the union of the lists of 128 / group consecutive tokens, times those tokens.  Lists that neighbours share cost what they hold.
- * Errors and *status as for vpp_chunk_attn_fwd.
+ * Errors and *status as for vpp_chunk_attn_fwd; VPP_DEV_BAD_BLOCK: a page that some token lists has an entry outside [0, num_blocks) (it is skipped).
  */
 size_t vpp_block_attn_workspace_size(const vpp_chunk_attn_args *args, int32_t topk);
 vpp_status vpp_block_attn_fwd(const vpp_chunk_attn_args *args, const int32_t *block_indices, int32_t topk, vpp_stream_t stream);

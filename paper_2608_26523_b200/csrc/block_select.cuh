@@ -18,7 +18,7 @@
 //  * block_few_kernel: tokens of requests of up to kSelectFew -- decode rows -- multiplied by warps from the registers that the loads fill, the scores in
 //    shared memory: there reading the means is all.
 //  * block_pick_kernel: a warp a (token, kv-head) ranks the candidates and settles the border.
-// 8192 tokens of 64/4 heads, 1152 pages, lists of 32: 122 us, of which the filter takes 88: 26 reading 134 MB of q (21 at the copy rate), then 18 steps of 2.4 (maxima)
+// 8192 tokens of 64/4 heads, 1152 pages, lists of 32: 124 us, of which the filter takes 88: 26 reading 134 MB of q (21 at the copy rate), then 18 steps of 2.4 (maxima)
 // and 4.4 thousand clk (lists), where the products take 2.05; its issue slots bound it, the lists' stores most.  One row of twenty has pages too close for 32 bits (8 us).
 // Before: all scores written down once, 4.6 KB a token and kv-head, and picked from there, 420 us; items of 128 tokens, eight warps that do one thing after the
 // other, two an SM, 195; items of 224 tokens, 148 of them, 130; means fetched and bounded by the four other warps alone, 3900 clk a step for 64 copies.
@@ -68,6 +68,7 @@ struct SelectParams {
     int row0, row1;               // this slab's tokens
     int run_pages, runs;          // pages of an item (a multiple of 128), items along a row
     int group_pages;              // pages of a group of which the maximum is kept (4, 2, 1; 0: 64 groups of every 64th page or so, in registers)
+    int item_tokens;              // of an item, at most
     int cap;                      // candidates of half an item's pages, at most
     SelectCandidate* found;       // [row1 - row0, Hkv, runs, 2, cap]
     int32_t* counts;              // [row1 - row0, Hkv, runs, 2] (past cap: more than fit)
@@ -396,7 +397,7 @@ __global__ void __launch_bounds__(kSelectThreads + 128, 1) block_filter_kernel(c
     block_scan<kAll>(p.num_reqs, 0x7fffffffu, first_item, false, [&](int r, bool&) {
         int lo;
         const int n = slab_rows(p, cu, r, lo);
-        return n > kSelectFew ? (n + kSelectItem - 1) / kSelectItem : 0;      // (the others: block_few_kernel)
+        return n > kSelectFew ? (n + p.item_tokens - 1) / p.item_tokens : 0;      // (the others: block_few_kernel)
     });
     const int run = item % p.runs, tg = item / p.runs, g = tg % p.num_kv_heads, tile = tg / p.num_kv_heads;
     if (tile >= first_item[p.num_reqs]) {
@@ -406,8 +407,8 @@ __global__ void __launch_bounds__(kSelectThreads + 128, 1) block_filter_kernel(c
     const int r = request_of(first_item, p.num_reqs, tile);
     int lo;
     const int rows_r = slab_rows(p, cu, r, lo);
-    const int row = lo + (tile - first_item[r]) * kSelectItem;
-    const int n = min(kSelectItem, lo + rows_r - row);
+    const int row = lo + (tile - first_item[r]) * p.item_tokens;
+    const int n = min(min(p.item_tokens, kSelectItem), lo + rows_r - row);      // (kSelectItem: what the compiler unrolls for)
     const int pos0 = p.prefix_len[r] + (row - cu[r]);
     const int end = select_end(p, (pos0 + n - 1) >> p.block_shift);      // of the item's last token
     // a page run that nobody needs: below the first candidate, past the last, or no token has more pages than it may list
@@ -568,7 +569,7 @@ __global__ void __launch_bounds__(kSelectThreads + 128, 1) block_filter_kernel(c
     // warps 0-3 and 4-7: the first 128 tokens, left and right halves of a step's pages; warps 8-15: the other tokens
     const int my_row = (warp >> 3) * 128 + (warp & 3) * 32 + lane, half = (warp >> 2) & 1;
     const uint32_t tD = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + (warp >> 3) * 128 + half * 64;
-    const bool tile_lives = (warp >> 3) * 128 < n;
+    const bool lives = (warp >> 3) * 128 + (warp & 3) * 32 < n;      // (the warp has a token)
     const int stop = my_row < n ? end_of(my_row) : 0;
     const int gp = p.group_pages, row_groups = gp > 0 ? p.run_pages / gp : 0;
     float* const my_maxima = p.maxima + (static_cast<long long>(item) * kSelectItem + my_row) * row_groups;
@@ -600,7 +601,7 @@ __global__ void __launch_bounds__(kSelectThreads + 128, 1) block_filter_kernel(c
         if (!borders) fetch(j + 2);
         const bool first_pass = filter && j < per_pass;
         tc_fence_after();
-        if (alive && tile_lives) {
+        if (alive && lives) {
             const int k0 = page0 + first_page(j) + half * 64;
             uint32_t sc[2][16];                 // 16 pages at a time, k of the first
             auto mask = [&](uint32_t (&s)[16], int k) {      // those that are no candidates: -inf
@@ -862,6 +863,38 @@ __device__ __forceinline__ bool pick_settle(PickScratch& s, const PickRow& w, in
     return true;
 }
 
+// Leaves of the m gathered entries those that may be among the need best of these and others, and returns how many.  (Runs' lists may be more than fit.)
+__device__ __noinline__ int pick_prune(PickScratch& s, int m, int need, float delta) {
+    const int lane = threadIdx.x & 31;
+    uint32_t border = 0;                 // (a little below the need-th best will do)
+    for (int b = 31; b >= 8; --b) {
+        const uint32_t c = border | (1u << b);
+        int k = 0;
+        for (int i = lane; i < m; i += 32) k += order_key(s.score[i]) >= c;
+        const int all = static_cast<int>(__reduce_add_sync(0xffffffffu, k));
+        if (all >= need) border = c;
+        if (all == need) break;
+    }
+    if (border < 0x00800000u) return m;  // (fewer than need)
+    const float lo = key_value(border) - 2.f * delta;
+    int kept = 0;
+    for (int i0 = 0; i0 < m; i0 += 32) {
+        const int i = i0 + lane;
+        const float score = i < m ? s.score[i] : 0.f;
+        const int page = i < m ? s.page[i] : 0;
+        const bool take = i < m && score >= lo;
+        const uint32_t t = __ballot_sync(0xffffffffu, take);
+        if (take) {
+            const int at = kept + __popc(t & ((1u << lane) - 1));
+            s.score[at] = score;
+            s.page[at] = page;
+        }
+        kept += __popc(t);
+        __syncwarp();
+    }
+    return kept;
+}
+
 // What the common path does not settle -- infinite or NaN scores, more candidates than fit (many pages that are (nearly) the same): all pages' scores in 64
 // bits, 128 at a time, each time joined with the best so far.
 __device__ __noinline__ void pick_thorough(PickScratch& s, PickRow w, int begin, int end, int need) {
@@ -1052,28 +1085,31 @@ __global__ void __launch_bounds__(kPickThreads, 3) block_pick_kernel(const Selec
             // (a run whose scores are all 0 lists none)
             odd = __any_sync(0xffffffffu, c > p.cap || (k < 2 * runs && !(p.bounds[static_cast<long long>(i) * p.runs + (k >> 1)] > 0.f)));
             for (int l0 = 0; l0 < min(32, 2 * runs - k0) && !odd; l0 += 4) {
-                int count[4], at[4];
+                int count[4];
                 SelectCandidate x[4];
 #pragma unroll
                 for (int l = 0; l < 4; ++l) {      // (four lists' first 32 under way at a time)
                     count[l] = __shfl_sync(0xffffffffu, c, l0 + l);
-                    at[l] = m;
-                    m += count[l];
                     if (lane < count[l]) x[l] = p.found[(static_cast<long long>(i) * p.runs * 2 + k0 + l0 + l) * p.cap + lane];
                 }
-                odd = m > kPickGather;
-                if (odd) break;
 #pragma unroll
                 for (int l = 0; l < 4; ++l) {
+                    if (m + count[l] > kPickGather) {
+                        __syncwarp();
+                        m = pick_prune(s, m, need, delta);
+                        odd |= m + count[l] > kPickGather;
+                        if (odd) break;
+                    }
                     if (lane < count[l]) {
-                        s.score[at[l] + lane] = x[l].score;
-                        s.page[at[l] + lane] = x[l].page;
+                        s.score[m + lane] = x[l].score;
+                        s.page[m + lane] = x[l].page;
                     }
                     for (int j = lane + 32; j < count[l]; j += 32) {
                         const SelectCandidate y = p.found[(static_cast<long long>(i) * p.runs * 2 + k0 + l0 + l) * p.cap + j];
-                        s.score[at[l] + j] = y.score;
-                        s.page[at[l] + j] = y.page;
+                        s.score[m + j] = y.score;
+                        s.page[m + j] = y.page;
                     }
+                    m += count[l];
                 }
             }
         }

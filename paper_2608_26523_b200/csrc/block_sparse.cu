@@ -89,6 +89,7 @@ struct SelectPlan {
     int slab;                   // tokens of a slab
     int run_pages, runs;        // pages of an item, items along a row
     int group_pages, cap;
+    int item_tokens;            // most tokens of an item
     int many_items, few_items;  // most items of a slab: of up to 256 tokens; of one
     size_t found, counts, bounds, maxima, bad, total;
 };
@@ -106,7 +107,12 @@ vpp_status select_plan(const vpp_block_select_args* a, SelectPlan* s) {
     if (a->num_first < 0 || a->num_last < 1 || a->num_first > a->topk || a->num_last > a->topk - a->num_first)
         return fail(VPP_ERR_INVALID_ARG, "need num_first >= 0, num_last >= 1 and num_first + num_last <= topk");
     const long long T = a->total_q > 0 ? a->total_q : 1, H = a->num_kv_heads, N = vpp::kSelectTile;
-    const long long I = vpp::kSelectItem, steps = (a->max_seq_len / a->block_size + N) / N;       // of 128 pages along a row
+    const long long sms = sm_count_or_default(), steps = (a->max_seq_len / a->block_size + N) / N;       // of 128 pages along a row
+    auto tiles_of = [&](long long rows, long long item) {
+        const long long tiles = (rows + a->num_reqs * (item - 1)) / item;      // (every request rounds up)
+        return tiles < rows ? tiles : rows;                                    // (every tile has a token)
+    };
+    long long I = vpp::kSelectItem;
     const int need = a->topk - a->num_first - a->num_last;
     // A border that is the need-th largest of the maxima of groups lets through about need (1 + need * group / (2 * pages)) pages.  Rows of few pages
     // list them all, others have pages enough for twice as many groups as are needed.
@@ -115,35 +121,38 @@ vpp_status select_plan(const vpp_block_select_args* a, SelectPlan* s) {
     s->cap = need <= 128 ? 128 : 256;
     // Launches of no more tokens than requests, or of a few tokens: decode rows alone, an item a token.
     const bool few_only = T <= a->num_reqs || T <= vpp::kSelectFew;
-    auto many_of = [&](long long rows) {
-        const long long tiles = (rows + a->num_reqs * (I - 1)) / I;      // (every request rounds up)
-        return few_only ? 0 : tiles < rows ? tiles : rows;           // (every tile has a token)
-    };
     const long long few = few_only ? T : a->num_reqs > 1 ? static_cast<long long>(a->num_reqs) * vpp::kSelectFew : 0;
     // Runs of pages, each of which lists its own best: one where the items fill half of the SMs, else as many as fill them all, of 1024 pages or more (decode rows: those
     // are read in 5 us) or 256.
-    const long long work = (few_only ? few : many_of(T)) * H, sms = sm_count_or_default();
+    const long long work = (few_only ? few : tiles_of(T, I)) * H;
     long long runs = work > 0 ? sms / work : 1;
     const long long shortest = few_only ? 8 : 2;
     if (runs > steps / shortest) runs = steps / shortest;
+    // (each lists what is needed and a few more, and block_pick_kernel gathers 512 at a time)
+    const long long gathered = 2 * 512 / (3 * (need > 0 ? need : 1));
+    if (runs > gathered) runs = gathered;
     const long long least = (steps * N + vpp::kSelectMaxRun - 1) / vpp::kSelectMaxRun;
     if (runs < least) runs = least;
     if (runs < 1) runs = 1;
+    // Tokens of an item: 256, or fewer where there are SMs for twice as many items all the same (few pages: 3150 tokens of 8/1 heads, 150 pages 60 -> 34 us.  Instead of
+    // runs it does not pay: 506 tokens of 32/8 heads, 1539 pages 52 -> 83).
+    while (I > 32 && tiles_of(T, I / 2) * H * runs <= sms) I /= 2;
+    s->item_tokens = static_cast<int>(I);
     s->run_pages = static_cast<int>((steps + runs - 1) / runs * N);
     s->runs = static_cast<int>((steps * N + s->run_pages - 1) / s->run_pages);
     const long long list = s->runs * (2ll * s->cap * static_cast<long long>(sizeof(vpp::SelectCandidate)) + 12);     // bytes of a row
-    const long long item = s->group_pages > 0 ? I * (s->run_pages / s->group_pages) * 4 : 0;                        // of an item
+    const long long item = s->group_pages > 0 ? vpp::kSelectItem * (s->run_pages / s->group_pages) * 4 : 0;                        // of an item
     long long slab = vpp::kSelectSlabBytes / (H * (list + item * s->runs / I));
     slab = slab / I * I;                              // (whole items of a long chunk)
     if (slab < I) slab = I;
     if (slab > T) slab = T;
     s->slab = static_cast<int>(slab);
-    const long long many = many_of(slab) * H * s->runs, few_items = (few_only ? slab : few) * H * s->runs;
+    const long long many = (few_only ? 0 : tiles_of(slab, I)) * H * s->runs, few_items = (few_only ? slab : few) * H * s->runs;
     if (many + few_items > INT32_MAX) return fail(VPP_ERR_UNSUPPORTED, "too many requests times heads");
     s->many_items = static_cast<int>(many);
     s->few_items = static_cast<int>(few_items);
     const size_t rows = static_cast<size_t>(slab) * H * s->runs;
-    if (rows > UINT32_MAX / (2 * s->cap * sizeof(vpp::SelectCandidate)))            // (byte offsets of candidates have 32 bits)
+    if (rows > UINT32_MAX / (2 * s->cap * sizeof(vpp::SelectCandidate)))            // (4 GiB: nobody has so many pages)
         return fail(VPP_ERR_UNSUPPORTED, "too many kv-heads times pages of max_seq_len");
     s->found = 0;
     s->counts = align_up(rows * 2 * s->cap * sizeof(vpp::SelectCandidate), 256);
@@ -403,6 +412,7 @@ vpp_status vpp_block_select(const vpp_block_select_args* a, vpp_stream_t stream_
     p.run_pages = s.run_pages;
     p.runs = s.runs;
     p.group_pages = s.group_pages;
+    p.item_tokens = s.item_tokens;
     p.cap = s.cap;
     p.found = reinterpret_cast<vpp::SelectCandidate*>(ws + s.found);
     p.counts = reinterpret_cast<int32_t*>(ws + s.counts);
@@ -433,7 +443,7 @@ vpp_status vpp_block_select(const vpp_block_select_args* a, vpp_stream_t stream_
         if (ce != cudaSuccess) return fail(VPP_ERR_CUDA, "page scores launch: %s", cudaGetErrorString(ce));
         const long long rows = static_cast<long long>(p.row1 - p.row0) * a->num_kv_heads, warps = vpp::kPickThreads / 32;
         long long blocks = (rows + warps - 1) / warps;
-        const long long cap = 3ll * sm_count_or_default();          // (those that fit at a time; 8: 128 instead of 125 us of 8192 tokens, the last wave half empty)
+        const long long cap = 3ll * sm_count_or_default();          // (those that fit at a time; 8: 3 us more of 8192 tokens, the last wave half empty)
         if (blocks > cap) blocks = cap;
         const int work_blocks = static_cast<int>(blocks);
         ce = launch(vpp::block_pick_kernel, static_cast<unsigned>(work_blocks + (a->status ? 1 : 0)), vpp::kPickThreads, smem_pick, stream, p, work_blocks);

@@ -250,3 +250,13 @@ def test_no_more_tokens_than_requests_but_a_request_with_most_of_them():
         gen = generator(11)
         table, pool = paged(gen, prefix, chunk, page)
         check(randn(gen, sum(chunk), 8, 128), randn(gen, pool, 2, 128), table, prefix, chunk, page, 12, 1, 2)
+
+
+@pytest.mark.parametrize("chunk", [[2, 1], [30, 3]])
+@pytest.mark.parametrize("topk, first, last", [(256, 0, 1), (140, 3, 2)])
+def test_more_listed_by_the_runs_than_is_gathered_at_a_time(chunk, topk, first, last):
+    """Rows of more than 8192 pages: three runs, each of which lists `topk` and more."""
+    prefix = [140000, 131050]
+    gen = generator(12)
+    table, pool = paged(gen, prefix, chunk, 16)
+    check(randn(gen, sum(chunk), 4, 128), randn(gen, pool, 1, 128), table, prefix, chunk, 16, topk, first, last)
