@@ -19,7 +19,7 @@
 //    shared memory: there reading the means is all.
 //  * block_pick_kernel: a warp a (token, kv-head) ranks the candidates and settles the border.
 // 8192 tokens of 64/4 heads, 1152 pages, lists of 32: 124 us, of which the filter takes 88: 26 reading 134 MB of q (21 at the copy rate), then 18 steps of 2.4 (maxima)
-// and 4.4 thousand clk (lists), where the products take 2.05; its issue slots bound it, the lists' stores most.  One row of twenty has pages too close for 32 bits (8 us).
+// and 4.4 thousand clk (lists), where the products take 2.05; of its issue slots 48 %, of the tensor pipe 24 %.  One row of twenty has pages too close for 32 bits (8 us).
 // Before: all scores written down once, 4.6 KB a token and kv-head, and picked from there, 420 us; items of 128 tokens, eight warps that do one thing after the
 // other, two an SM, 195; items of 224 tokens, 148 of them, 130; means fetched and bounded by the four other warps alone, 3900 clk a step for 64 copies.
 #pragma once
