@@ -173,7 +173,7 @@ __device__ __forceinline__ void mma_16x8(float (&d)[4], uint32_t a0, uint32_t a1
 // with few instructions: 16 pages a warp and round, multiplied by small matrix instructions straight from the registers that the loads fill (each lane's features are a
 // permutation of the product's inner index that the other operand shares).  The columns of that operand are the two parts of the summed query, and for the absolute
 // products that bound the error -- the same registers without signs -- those of the parts and of sum_h |q_h|.  (Dot products in registers, eight lanes a page: 400 instructions
-// for 16 pages instead of 70; 16 rows of 64/4 heads with 2300 pages took 32 us with the page selection behind it, and take 27.)
+// for 16 pages instead of 70; 16 rows of 64/8 heads, up to 2048 pages, took 32 us with block_pick_kernel behind it, and take 26.)
 __global__ void __launch_bounds__(kFewThreads) block_few_kernel(const SelectParams p, const int by_token) {
     extern __shared__ float s_score[];                              // [run_pages], then cu [num_reqs + 1]
     constexpr int kWarps = kFewThreads / 32;
