@@ -15,7 +15,7 @@
 //    products run under this one's scores.  They are formed twice: the first time the maxima of groups
 //    of pages are kept, whose need-th largest bounds a token's border from below; the second time what is not below that by more than the error
 //    bound -- a few more pages than needed -- is written down, a thread a token and half of the pages.
-//  * block_few_kernel: tokens of requests of up to kSelectFew -- decode rows -- multiplied by warps from the registers that the loads fill, the scores in
+//  * block_few_kernel: tokens of requests of up to kSelectFew in the slab -- decode rows, a last rest -- multiplied by warps from the registers that the loads fill, the scores in
 //    shared memory: there reading the means is all.
 //  * block_pick_kernel: a warp a (token, kv-head) ranks the candidates and settles the border.
 // 8192 tokens of 64/4 heads, 1152 pages, lists of 32: 124 us, of which the filter takes 88: 26 reading 134 MB of q (21 at the copy rate), then 18 steps of 2.4 (maxima)
@@ -1083,7 +1083,7 @@ __global__ void __launch_bounds__(kPickThreads, 3) block_pick_kernel(const Selec
         for (int k0 = 2 * run0; k0 < 2 * runs && !odd; k0 += 32) {
             const int k = k0 + lane, c = k < 2 * runs ? p.counts[static_cast<long long>(i) * p.runs * 2 + k] : 0;
             // (a run whose scores are all 0 lists none)
-            odd = __any_sync(0xffffffffu, c > p.cap || (k < 2 * runs && !(p.bounds[static_cast<long long>(i) * p.runs + (k >> 1)] > 0.f)));
+            odd = __any_sync(0xffffffffu, static_cast<uint32_t>(c) > static_cast<uint32_t>(p.cap) || (k < 2 * runs && !(p.bounds[static_cast<long long>(i) * p.runs + (k >> 1)] > 0.f)));
             for (int l0 = 0; l0 < min(32, 2 * runs - k0) && !odd; l0 += 4) {
                 int count[4];
                 SelectCandidate x[4];

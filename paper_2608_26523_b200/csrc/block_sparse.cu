@@ -121,7 +121,7 @@ vpp_status select_plan(const vpp_block_select_args* a, SelectPlan* s) {
     s->cap = need <= 128 ? 128 : 256;
     // Launches of no more tokens than requests, or of a few tokens: decode rows alone, an item a token.
     const bool few_only = T <= a->num_reqs || T <= vpp::kSelectFew;
-    const long long few = few_only ? T : a->num_reqs > 1 ? static_cast<long long>(a->num_reqs) * vpp::kSelectFew : 0;
+    long long few = few_only ? T : a->num_reqs > 1 ? static_cast<long long>(a->num_reqs) * vpp::kSelectFew : 0;
     // Runs of pages, each of which lists its own best: one where the items fill half of the SMs, else as many as fill them all, of 1024 pages or more (decode rows: those
     // are read in 5 us) or 256.
     const long long work = (few_only ? few : tiles_of(T, I)) * H;
@@ -147,6 +147,8 @@ vpp_status select_plan(const vpp_block_select_args* a, SelectPlan* s) {
     if (slab < I) slab = I;
     if (slab > T) slab = T;
     s->slab = static_cast<int>(slab);
+    // (a request by itself has few rows only in a last slab that is a rest of so many)
+    if (few == 0 && T % slab >= 1 && T % slab <= vpp::kSelectFew) few = vpp::kSelectFew;
     const long long many = (few_only ? 0 : tiles_of(slab, I)) * H * s->runs, few_items = (few_only ? slab : few) * H * s->runs;
     if (many + few_items > INT32_MAX) return fail(VPP_ERR_UNSUPPORTED, "too many requests times heads");
     s->many_items = static_cast<int>(many);
