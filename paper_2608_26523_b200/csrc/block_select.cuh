@@ -46,8 +46,9 @@ constexpr int kSelectMaxTopk = 256;
 constexpr int kSelectMaxRun = 4096;           // pages of an item: their scores, or their places, are kept in shared memory
 constexpr int kSelectA = 2 * 2 * kSelectTile * 128;   // an accumulator's operand: two bf16 parts of 128 x 128, two 64-feature slabs each
 constexpr int kSelectB = 2 * kSelectTile * 128;
-constexpr int kSelectSmem = 2 * kSelectA + 2 * kSelectB + 1024 /* alignment */ + 4096 /* barriers, borders */;      // and the pages, the lengths
+constexpr int kSelectSmem = 2 * kSelectA + 2 * kSelectB + 1024 /* alignment */ + 4096 /* barriers, borders */;      // and the pages
 static_assert(kSelectSmem + 4 * kSelectMaxRun <= 232448 - 8 * 1024, "shared memory of one CTA");
+static_assert(2 * 4 * (kLengthsMaxReqs + 1) <= 2 * kSelectA, "the lengths fit where the operands come");
 
 // A page that may be among a token's best.
 struct __align__(8) SelectCandidate {
@@ -374,7 +375,7 @@ __global__ void __launch_bounds__(kSelectThreads + 128, 1) block_filter_kernel(c
     float* const s_weight = reinterpret_cast<float*>(sX + 64);         // [256] what a token's bound is made of
     float* const s_floor = s_weight + kSelectItem;                         // [256] lowest score of a candidate
     int32_t* const s_page = reinterpret_cast<int32_t*>(sX + 4096);     // [run_pages] physical page, -1: counts as 0
-    int32_t* const cu = s_page + p.run_pages;                          // [num_reqs + 1], then items before request r [num_reqs + 1]
+    int32_t* const cu = reinterpret_cast<int32_t*>(gen);               // [num_reqs + 1], then items before request r [num_reqs + 1]: until the queries come there
     int32_t* const first_item = cu + p.num_reqs + 1;
 
     if (tid == 0) {
@@ -440,6 +441,7 @@ __global__ void __launch_bounds__(kSelectThreads + 128, 1) block_filter_kernel(c
         if (bad) *s_badp = 1;
     }
     const int v = tid & 15;
+    __syncthreads();                      // (all have read their lengths)
     // ---- the group's queries, summed and split ----
     if (tid < kSelectThreads) {
         const uint8_t* const q0 = p.q + (static_cast<long long>(row) * p.num_q_heads + g * G) * 256 + v * 16;

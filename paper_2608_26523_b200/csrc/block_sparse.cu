@@ -426,13 +426,10 @@ vpp_status vpp_block_select(const vpp_block_select_args* a, vpp_stream_t stream_
     p.indices = a->indices;
     p.status = a->status;
     const size_t lens = sizeof(int32_t) * (static_cast<size_t>(a->num_reqs) + 1);
-    const size_t smem_many = vpp::kSelectSmem + 4 * static_cast<size_t>(s.run_pages) + 2 * lens, smem_pick = vpp::kPickSmem + lens;
+    const size_t smem_many = vpp::kSelectSmem + 4 * static_cast<size_t>(s.run_pages), smem_pick = vpp::kPickSmem + lens;
     const size_t smem_few = 4 * static_cast<size_t>(s.run_pages) + lens;
     cudaError_t ce = cudaSuccess;
-    if (s.many_items > 0) {
-        if (smem_many > 232448) return fail(VPP_ERR_UNSUPPORTED, "too many requests (%d) for chunks of this context length", a->num_reqs);
-        ce = cudaFuncSetAttribute(vpp::block_filter_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem_many));
-    }
+    if (s.many_items > 0) ce = cudaFuncSetAttribute(vpp::block_filter_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem_many));
     if (ce == cudaSuccess && s.few_items > 0) ce = cudaFuncSetAttribute(vpp::block_few_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem_few));
     if (ce == cudaSuccess) ce = cudaFuncSetAttribute(vpp::block_pick_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem_pick));
     if (ce != cudaSuccess) return fail(VPP_ERR_CUDA, "page selection attributes: %s", cudaGetErrorString(ce));
