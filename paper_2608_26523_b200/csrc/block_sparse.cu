@@ -17,6 +17,14 @@ using namespace vpp::host;
 
 namespace {
 
+// The dynamic shared memory that launches of a kernel may have: the most that any call's has, not this call's, for it holds for the launches of other host
+// threads too.
+constexpr int kLengthsMaxBytes = 4 * (vpp::kLengthsMaxReqs + 1);
+template <typename Kernel>
+cudaError_t allow_smem(Kernel kernel, int most) {
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
+}
+
 bool mis16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
 
 vpp_status check_rope(const vpp_rope_spec& r, int head_dim, int heads) {
@@ -364,7 +372,7 @@ vpp_status vpp_block_means(const vpp_block_means_args* a, vpp_stream_t stream_) 
     if (blocks > cap) blocks = cap;
     const int work_blocks = static_cast<int>(blocks);
     cudaError_t ce = cudaSuccess;
-    if (a->num_reqs > 4096) ce = cudaFuncSetAttribute(vpp::block_means_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * 4 * (vpp::kLengthsMaxReqs + 1));
+    if (a->num_reqs > 4096) ce = allow_smem(vpp::block_means_kernel, 2 * kLengthsMaxBytes);
     if (ce == cudaSuccess) ce = launch(vpp::block_means_kernel, static_cast<unsigned>(work_blocks + (a->status ? 1 : 0)), vpp::kMeansThreads,
                                   2 * sizeof(int32_t) * (static_cast<size_t>(a->num_reqs) + 1), stream, p, work_blocks);
     if (ce != cudaSuccess) return fail(VPP_ERR_CUDA, "page means launch: %s", cudaGetErrorString(ce));
@@ -429,9 +437,9 @@ vpp_status vpp_block_select(const vpp_block_select_args* a, vpp_stream_t stream_
     const size_t smem_many = vpp::kSelectSmem + 4 * static_cast<size_t>(s.run_pages), smem_pick = vpp::kPickSmem + lens;
     const size_t smem_few = 4 * static_cast<size_t>(s.run_pages) + lens;
     cudaError_t ce = cudaSuccess;
-    if (s.many_items > 0) ce = cudaFuncSetAttribute(vpp::block_filter_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem_many));
-    if (ce == cudaSuccess && s.few_items > 0) ce = cudaFuncSetAttribute(vpp::block_few_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem_few));
-    if (ce == cudaSuccess) ce = cudaFuncSetAttribute(vpp::block_pick_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem_pick));
+    if (s.many_items > 0) ce = allow_smem(vpp::block_filter_kernel, vpp::kSelectSmem + 4 * vpp::kSelectMaxRun);
+    if (ce == cudaSuccess && s.few_items > 0) ce = allow_smem(vpp::block_few_kernel, 4 * vpp::kSelectMaxRun + kLengthsMaxBytes);
+    if (ce == cudaSuccess) ce = allow_smem(vpp::block_pick_kernel, vpp::kPickSmem + kLengthsMaxBytes);
     if (ce != cudaSuccess) return fail(VPP_ERR_CUDA, "page selection attributes: %s", cudaGetErrorString(ce));
     for (int64_t row0 = 0; row0 < a->total_q; row0 += s.slab) {
         p.row0 = static_cast<int32_t>(row0);
@@ -520,8 +528,9 @@ vpp_status vpp_block_attn_fwd(const vpp_chunk_attn_args* a, const int32_t* block
     const int context = (a->max_seq_len + a->block_size - 1) / a->block_size, most = vpp::kBlkWindow / b.words;
     lp.window = context < 1 ? 1 : context < most ? context : most;
     const size_t lens = sizeof(int32_t) * (2 * (static_cast<size_t>(a->num_reqs) + 1) + static_cast<size_t>(lp.window) * (b.words + 1));
-    cudaError_t ce = cudaFuncSetAttribute(vpp::block_lists_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lens));
-    if (ce == cudaSuccess) ce = cudaFuncSetAttribute(vpp::attn_blk_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, vpp::kBlkSmem);
+    // (a window's masks and pages: most where a page's mask is one word)
+    cudaError_t ce = allow_smem(vpp::block_lists_kernel, 2 * kLengthsMaxBytes + 2 * 4 * vpp::kBlkWindow);
+    if (ce == cudaSuccess) ce = allow_smem(vpp::attn_blk_kernel, vpp::kBlkSmem);
     if (ce != cudaSuccess) return fail(VPP_ERR_CUDA, "block-sparse attention attributes: %s", cudaGetErrorString(ce));
     const unsigned tiles = static_cast<unsigned>(b.max_tiles) * a->num_kv_heads;
     ce = launch(vpp::block_lists_kernel, tiles, vpp::kBlkListThreads, lens, stream, lp);
