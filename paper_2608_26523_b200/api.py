@@ -408,13 +408,21 @@ def vpp_block_means(k_cache, k_means, block_table, prefix_len, chunk_len, block_
         _check(rc)
 
 
-def vpp_block_select_workspace_size(total_q, num_reqs, num_q_heads, num_kv_heads, block_size, max_seq_len, topk=None):
-    """Bytes of workspace of vpp_block_select; topk None: enough for every topk."""
-    def size(k):
-        a = BlockSelectArgs(num_reqs=int(num_reqs), block_size=int(block_size), total_q=int(total_q), max_seq_len=int(max_seq_len),
-                            num_q_heads=int(num_q_heads), num_kv_heads=int(num_kv_heads), head_dim=128, topk=k, num_first=0, num_last=1)
+def vpp_block_select_workspace_size(total_q, num_reqs, num_q_heads, num_kv_heads, block_size, max_seq_len, topk=None, num_first=None, num_last=None):
+    """Bytes of workspace of a vpp_block_select of these sizes.  topk None: enough for every topk; num_first or num_last None: for every one that topk allows."""
+    a = BlockSelectArgs(num_reqs=int(num_reqs), block_size=int(block_size), total_q=int(total_q), max_seq_len=int(max_seq_len),
+                        num_q_heads=int(num_q_heads), num_kv_heads=int(num_kv_heads), head_dim=128)
+
+    def size(topk, first, last):
+        a.topk, a.num_first, a.num_last = topk, first, last
         return int(load_library().vpp_block_select_workspace_size(ctypes.byref(a)))
-    return size(int(topk)) if topk is not None else max(size(k) for k in (1, 64, 128, 256))
+    topk = 256 if topk is None else int(topk)
+    first, last = 0 if num_first is None else int(num_first), 1 if num_last is None else int(num_last)
+    most = size(topk, first, last)
+    if most == 0 or (num_first is not None and num_last is not None):
+        return most
+    # the size goes by the number of pages to pick, and neither up nor down with it
+    return max(size(picks + 1, 0, 1) for picks in range(topk - first - last + 1))
 
 
 def vpp_block_select(q, k_means, block_table, prefix_len, chunk_len, block_size, max_seq_len, indices, workspace, num_first=0, num_last=1,

@@ -19,7 +19,7 @@ def check(seed, prefix, T, hq, hkv, page, topk, max_seq, fill, rows, calls=1):
     pool = width + 3
     table = torch.randperm(pool, generator=gen, device="cuda")[:width].to(torch.int32).view(1, width)
     q, means = randn(gen, T, hq, 128), randn(gen, pool, hkv, 128)
-    size = api.vpp_block_select_workspace_size(T, 1, hq, hkv, page, max_seq, topk=topk - FIRST - LAST + 1)      # (as many pages to pick as the call has)
+    size = api.vpp_block_select_workspace_size(T, 1, hq, hkv, page, max_seq, topk, FIRST, LAST)
     ws = torch.empty(size, dtype=torch.uint8, device="cuda").fill_(fill)
     got = torch.full((T, hkv, topk), -77, dtype=torch.int32, device="cuda")
     for _ in range(calls):
