@@ -515,168 +515,6 @@ vpp_status vpp_block_means(const vpp_block_means_args *args, vpp_stream_t stream
  * Candidates are kept for up to 128 MiB worth of tokens at a time, or for 256 tokens where those take more (hundreds of kv-heads; dozens of them with more than 32
  * of tens of thousands of pages to pick; millions of pages): the workspace grows no further with the chunk.  Past 4 GiB VPP_ERR_UNSUPPORTED.  Its size is not
  * monotone in topk, num_first, num_last or total_q (fewer may need more): ask for every combination that the calls of one workspace have.
- * Returns after enqueueing two or three kernels on `stream`; no allocation, no synchronisation.
- */
-typedef struct {
-    const void *q;
-    const void *kv_cache;
-    int64_t kv_row_stride;
-    const int32_t *indices;
-    int32_t topk;
-    const int32_t *block_table;
-    const int32_t *prefix_len;
-    const int32_t *chunk_len;
-    int32_t num_reqs;
-    int32_t max_blocks_per_req;
-    int32_t block_size;
-    int32_t num_blocks;
-    int32_t total_q;
-    int32_t max_seq_len;
-    int32_t num_q_heads;
-    float softmax_scale;
-    void *out;
-    float *lse;
-    void *workspace;
-    size_t workspace_bytes;
-    int32_t *status;
-} vpp_sparse_attn_args;
-
-size_t vpp_sparse_attn_workspace_size(int32_t total_q);
-vpp_status vpp_sparse_mla_fwd(const vpp_sparse_attn_args *args, vpp_stream_t stream);
-
-/*
- * Rotary positions: how a row's features are turned to the row's position (the step before the append of a layer).
- * With pos the absolute position prefix_len[r] + i of row i of request r, pair j of the rotated part (a, b) becomes
- *     a' = amplitude * (a cos(pos * inv_freq[j]) - b sin(pos * inv_freq[j]))
- *     b' = amplitude * (b cos(pos * inv_freq[j]) + a sin(pos * inv_freq[j]))
- * for j in [0, rot_dim / 2); the features before rot_offset and from rot_offset + rot_dim on are copied.  Angles are formed in 64 bits (a
- * position of a million loses 0.03 rad in 32), products in 32, and results are rounded once.
- *
- * inv_freq     float [rot_dim / 2], device: the caller's frequencies, whatever scaling for long contexts they carry.
- * rot_dim      a multiple of 16, at most 256 (other values: VPP_ERR_UNSUPPORTED).
- * rot_offset   first rotated feature, a multiple of 8; rot_offset + rot_dim <= head_dim.
- * layout       VPP_ROPE_HALF: pair j is features j and j + rot_dim / 2 of the rotated part; VPP_ROPE_INTERLEAVED: 2 j and 2 j + 1.
- * amplitude    finite; 1 where the scaling has no factor of its own.
- */
-enum { VPP_ROPE_HALF = 0, VPP_ROPE_INTERLEAVED = 1 };
-typedef struct {
-    const float *inv_freq;
-    int32_t rot_dim;
-    int32_t rot_offset;
-    int32_t layout;
-    float amplitude;
-} vpp_rope_spec;
-
-/*
- * Rotation of total_q rows of num_heads heads, packed request-major like q.
- *
- * x, out       bf16; element (row t, head h, feature d) at t*token_stride + h*head_stride + d (strides in ELEMENTS, multiples of 8, feature stride 1;
- *              16-byte aligned), so that either may be a part of wider rows (a fused projection's, the rotated part of an
- *              absorbed query).  out may be x itself with the same strides; otherwise they must not overlap.
- * head_dim     a multiple of 16, at most 1024; num_heads at most 65536; num_reqs at most 8192.
- * status       optional device int32, zeroed by the call; VPP_DEV_BAD_LENGTHS: a negative length, a position past 2^31 - 1 or
- *              sum(chunk_len) != total_q -- nothing is written.
- * Returns after enqueueing one kernel on `stream`.
- */
-typedef struct {
-    const void *x;
-    void *out;
-    int64_t x_token_stride, x_head_stride;
-    int64_t out_token_stride, out_head_stride;
-    const int32_t *prefix_len;
-    const int32_t *chunk_len;
-    int32_t num_reqs;
-    int32_t total_q;
-    int32_t num_heads;
-    int32_t head_dim;
-    vpp_rope_spec rope;
-    int32_t *status;
-} vpp_rope_args;
-
-vpp_status vpp_rope(const vpp_rope_args *args, vpp_stream_t stream);
-
-/*
- * vpp_kv_append with the rotation on the way: row i of request r goes to its position in the cache with its keys rotated
- * (values are copied), and, if q is given, the same rows' queries are rotated into q_out -- one kernel, one pass over the new rows.
- *
- * append       as for vpp_kv_append, except that k_new and v_new have strides: element (row t, head h, feature d) at
- *              t*token_stride + h*head_stride + d (ELEMENTS, multiples of 8).  v_new NULL: keys only (absorbed MLA).  head_dim_qk and
- *              head_dim_v must be multiples of 16, at most 1024, and heads at most 65536.
- * q, q_out     bf16 rows of num_q_heads heads of head_dim_qk features with their own strides; both NULL: no queries.  q_out may be q with the
- *              same strides; otherwise neither may overlap any other buffer of the call.
- * status       as for vpp_kv_append; with VPP_DEV_BAD_BLOCK the row's queries are still rotated.
- */
-typedef struct {
-    vpp_kv_append_args append;
-    int64_t k_new_token_stride, k_new_head_stride;
-    int64_t v_new_token_stride, v_new_head_stride;
-    const void *q;
-    void *q_out;
-    int64_t q_token_stride, q_head_stride;
-    int64_t q_out_token_stride, q_out_head_stride;
-    int32_t num_q_heads;
-    vpp_rope_spec rope;
-} vpp_kv_append_rope_args;
-
-vpp_status vpp_kv_append_rope(const vpp_kv_append_rope_args *args, vpp_stream_t stream);
-
-/*
- * Block-sparse attention over a paged cache: what bounds the cost of a long prefix for models with ordinary key/value heads, as index-selected
- * attention (vpp_sparse_mla_fwd) does for absorbed MLA (the paper's "Impact of Sparse Attention").  Pages of the cache are the
- * blocks.  Three calls a step, after the append:
- *   vpp_block_means    the mean key of every page that the chunk completes
- *   vpp_block_select   for every token and kv-head, the pages whose mean keys its queries score highest
- *   vpp_block_attn_fwd Eq. 1 over the listed pages
- *
- * vpp_block_means: page j of request r is completed by the call with prefix_len <= (j + 1) * block_size - 1 < prefix_len + chunk_len; the mean over
- * its block_size keys (formed in 32 bits, rounded to bf16) goes to k_means at its physical page.  (prefix_len = 0 and chunk_len = the
- * context's length form those of a whole context, as for a prefix that was cached without them.)
- *
- * k_cache, strides, block_table (required), prefix_len, chunk_len, num_reqs (<= 8192), max_blocks_per_req, block_size (a power of two), num_blocks,
- * total_q, num_kv_heads: as in vpp_chunk_attn_args; the cache already holds the chunk's keys.  head_dim 128.
- * k_means      bf16 [num_blocks, num_kv_heads, 128], dense, 16-byte aligned; other pages' rows are left as they are.
- * status       optional device int32, zeroed by the call; VPP_DEV_BAD_LENGTHS (nothing is written) or VPP_DEV_BAD_BLOCK (that page is skipped).
- */
-typedef struct {
-    const void *k_cache;
-    int64_t k_block_stride, k_token_stride, k_head_stride;
-    void *k_means;
-    const int32_t *block_table;
-    const int32_t *prefix_len;
-    const int32_t *chunk_len;
-    int32_t num_reqs;
-    int32_t max_blocks_per_req;
-    int32_t block_size;
-    int32_t num_blocks;
-    int32_t total_q;
-    int32_t num_kv_heads;
-    int32_t head_dim;
-    int32_t *status;
-} vpp_block_means_args;
-
-vpp_status vpp_block_means(const vpp_block_means_args *args, vpp_stream_t stream);
-
-/*
- * Page selection.  A token at position p of request r may attend to pages 0 .. c, c = p / block_size.  For kv-head g the score of page b is
- *     s(b) = sum over the q-heads h of g of <q_h, mean_b,g>        (mean_b,g: k_means at page b's physical place)
- * If c + 1 <= topk all pages are listed.  Otherwise the first num_first pages, the last num_last (the own page c among them), and of the others the
- * topk - num_first - num_last with the highest scores: ties go to the lowest index, NaN is below everything.  Lists ascend; -1 stands behind the
- * pages where there are fewer than topk.  The selection is that of the scores in 64 bits: where 32 bits cannot tell two pages apart the call
- * forms theirs again.  Means of the first num_first and the last num_last pages are not needed (but the entries must be valid); all the others before
- * the own page must be complete and have had their means written.
- *
- * q            bf16 [total_q, num_q_heads, 128], dense, packed request-major, 16-byte aligned (the rotated queries).
- * k_means, block_table (required), prefix_len, chunk_len, num_reqs (<= 8192), max_blocks_per_req, block_size (a power of two), num_blocks, total_q,
- * max_seq_len: as above and in vpp_chunk_attn_args.  num_q_heads / num_kv_heads at most 128.
- * topk         1 .. 256;  num_first >= 0, num_last >= 1, num_first + num_last <= topk.
- * indices      int32 [total_q, num_kv_heads, topk], written.
- * workspace    device memory of vpp_block_select_workspace_size(args) bytes, 256-byte aligned; contents need no initialisation.  Two calls that overlap
- *              on the GPU need two.
- * status       optional device int32, zeroed by the call; VPP_DEV_BAD_LENGTHS (nothing is written), VPP_DEV_BAD_BLOCK (a page that is scored has an entry
- *              outside [0, num_blocks): lists undefined, but in range) or VPP_DEV_TIMEOUT.
- * Candidates are kept for up to 128 MiB worth of tokens at a time: the workspace stays near that however long the chunk is (and goes above it only with hundreds of
- * kv-heads, or where max_seq_len has millions of pages; past 4 GiB VPP_ERR_UNSUPPORTED).  Its size goes neither up nor down with topk, num_first,
- * num_last and total_q alone: ask for every combination that calls with one workspace have.
  * Returns after enqueueing two or three kernels on `stream` for each of those portions of the tokens.
  */
 typedef struct {
