@@ -27,6 +27,7 @@
 
 #include <cstdint>
 
+#include "device_status.h"
 #include "lengths.cuh"
 #include "ptx.cuh"
 #include "rope.cuh"
@@ -1008,17 +1009,11 @@ __global__ void __launch_bounds__(kPickThreads, 3) block_pick_kernel(const Selec
     pdl_launch_dependents();
     pdl_wait();
     if (static_cast<int>(blockIdx.x) >= work_blocks) {
-        int worst = 0;
-        for (int i = tid; i < p.items; i += kPickThreads) {
-            const int b = p.bad[i];
-            worst = max(worst, b == 1 ? 8 : b == 3 ? 6 : b);       // (lengths before a timeout before a page)
-        }
-        const bool lengths = __syncthreads_or(worst == 8), late = __syncthreads_or(worst == 6), page = __syncthreads_or(worst == 2);
-        if (tid == 0) {
-            const int now = lengths ? 1 : late ? 3 : page ? 2 : 0;
-            if (p.row0 == 0) *p.status = now;
-            else if (now != 0 && *p.status == 0) *p.status = now;
-        }
+        int worst = 0, now = 0;
+        for (int i = tid; i < p.items; i += kPickThreads) worst = worse_status(worst, p.bad[i]);
+        for (int k = 1; k <= 3; ++k)
+            if (__syncthreads_or(worst == k)) now = worse_status(now, k);
+        if (tid == 0) *p.status = p.row0 == 0 ? now : worse_status(now, *p.status);
         return;
     }
     if (!scan_lengths<kPickThreads>(p.prefix_len, p.chunk_len, p.num_reqs, p.capacity, p.total_q, cu)) return;
@@ -1061,7 +1056,7 @@ __global__ void __launch_bounds__(kPickThreads, 3) block_pick_kernel(const Selec
         for (int k = lane; k < p.topk; k += 32)
             if (k < p.num_first || k >= p.num_first + need) out[k] = k < p.num_first ? k : own + 1 - (p.topk - k);
         if (need == 0) continue;
-        if (p.runs == 1 && now.delta > 0.f && now.delta < INFINITY && now.count.x <= 32 && now.count.y <= 32) {
+        if (p.runs == 1 && now.delta > 0.f && now.delta < INFINITY && now.count.x <= 32 && now.count.y <= 32 && now.count.x + now.count.y >= need) {
             pick_two(s, w, now.x, now.count.x, now.y, now.count.y, need, now.delta, out + p.num_first);
             __syncwarp();
             continue;
@@ -1116,6 +1111,7 @@ __global__ void __launch_bounds__(kPickThreads, 3) block_pick_kernel(const Selec
             }
         }
         __syncwarp();
+        odd |= m < need;                  // (a scoring block that gave up lists too few)
         if (odd || !pick_settle(s, w, m, need, delta)) pick_thorough(s, w, p.num_first, end, need);
         __syncwarp();
         // ascending
