@@ -515,7 +515,7 @@ vpp_status vpp_block_means(const vpp_block_means_args *args, vpp_stream_t stream
  * Candidates are kept for up to 128 MiB worth of tokens at a time, or for 256 tokens where those take more (hundreds of kv-heads; dozens of them with more than 32
  * of tens of thousands of pages to pick; millions of pages): the workspace grows no further with the chunk.  Past 4 GiB VPP_ERR_UNSUPPORTED.  Its size is not
  * monotone in topk, num_first, num_last or total_q (fewer may need more): ask for every combination that the calls of one workspace have.
- * Returns after enqueueing two or three kernels on `stream` for each of those portions of the tokens.
+ * Returns after enqueueing two or three kernels on `stream` for each of those portions of the tokens (one kernel where num_first + num_last = topk: no page is scored).
  */
 typedef struct {
     const void *q;

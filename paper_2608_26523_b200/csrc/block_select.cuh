@@ -68,7 +68,7 @@ struct SelectParams {
     int total_q, num_q_heads, num_kv_heads;
     int topk, num_first, num_last;
     int row0, row1;               // this slab's tokens
-    int run_pages, runs;          // pages of an item (a multiple of 128), items along a row
+    int run_pages, runs;          // pages of an item (a multiple of 128), items along a row (0: nothing is scored)
     int group_pages;              // pages of a group of which the maximum is kept (4, 2, 1; 0: 64 groups of every 64th page or so, in registers)
     int item_tokens;              // of an item, at most
     int cap;                      // candidates of half an item's pages, at most
@@ -1009,9 +1009,9 @@ __global__ void __launch_bounds__(kPickThreads, 3) block_pick_kernel(const Selec
     pdl_launch_dependents();
     pdl_wait();
     if (static_cast<int>(blockIdx.x) >= work_blocks) {
-        int worst = 0, now = 0;
+        int worst = 0, now = scan_lengths<kPickThreads>(p.prefix_len, p.chunk_len, p.num_reqs, p.capacity, p.total_q, cu) ? 0 : 1 /* VPP_DEV_BAD_LENGTHS */;
         for (int i = tid; i < p.items; i += kPickThreads) worst = worse_status(worst, p.bad[i]);
-        for (int k = 1; k <= 3; ++k)
+        for (int k = 2; k <= 3; ++k)      // (VPP_DEV_BAD_BLOCK, VPP_DEV_TIMEOUT)
             if (__syncthreads_or(worst == k)) now = worse_status(now, k);
         if (tid == 0) *p.status = p.row0 == 0 ? now : worse_status(now, *p.status);
         return;
@@ -1052,10 +1052,10 @@ __global__ void __launch_bounds__(kPickThreads, 3) block_pick_kernel(const Selec
         const PickRow w{p.q + (static_cast<long long>(t) * p.num_q_heads + g * G) * 256, p.block_table + static_cast<long long>(r) * p.max_blocks_per_req,
                         p.means + g * 256, static_cast<long long>(p.num_kv_heads) * 256, G, p.num_blocks};
         // (own + 1 > topk >= first + last: the two ends do not meet, and there are more candidates than needed)
-        const int end = select_end(p, own), run0 = p.num_first / p.run_pages, runs = (end + p.run_pages - 1) / p.run_pages;
         for (int k = lane; k < p.topk; k += 32)
             if (k < p.num_first || k >= p.num_first + need) out[k] = k < p.num_first ? k : own + 1 - (p.topk - k);
-        if (need == 0) continue;
+        if (need == 0) continue;          // (nothing was scored)
+        const int end = select_end(p, own), run0 = p.num_first / p.run_pages, runs = (end + p.run_pages - 1) / p.run_pages;
         if (p.runs == 1 && now.delta > 0.f && now.delta < INFINITY && now.count.x <= 32 && now.count.y <= 32 && now.count.x + now.count.y >= need) {
             pick_two(s, w, now.x, now.count.x, now.y, now.count.y, need, now.delta, out + p.num_first);
             __syncwarp();

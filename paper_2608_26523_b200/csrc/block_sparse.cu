@@ -122,6 +122,13 @@ vpp_status select_plan(const vpp_block_select_args* a, SelectPlan* s) {
     };
     long long I = vpp::kSelectItem;
     const int need = a->topk - a->num_first - a->num_last;
+    if (need == 0) {          // no page is scored: lists by position alone
+        *s = SelectPlan{};
+        s->slab = static_cast<int>(T * H <= 1 << 30 ? T : (1 << 30) / H);
+        s->run_pages = vpp::kSelectTile;
+        s->total = 256;
+        return VPP_OK;
+    }
     // A border that is the need-th largest of the maxima of groups lets through about need (1 + need * group / (2 * pages)) pages.  Rows of few pages
     // list them all, others have pages enough for twice as many groups as are needed.
     // (Up to 32 are needed: 64 groups, kept in registers.)

@@ -33,3 +33,26 @@ def test_chunks_among_thousands_of_requests(R):
         r = int(np.searchsorted(cu, t, side="right")) - 1
         want = ref_block_select(q64[t:t + 1], m64, table[r:r + 1].cpu().numpy(), [int(prefix[r]) + t - int(cu[r])], [1], page, topk, first, last)
         assert (got[t] == want[0]).all(), (t, r)
+
+
+@pytest.mark.parametrize("prefix, chunk", [([900, 0, 333], [1, 1, 1]), ([900, 0, 333], [300, 20, 1]), ([3000], [4])])
+@pytest.mark.parametrize("topk, first", [(1, 0), (4, 2), (200, 3)])
+def test_lists_by_position_alone(prefix, chunk, topk, first):
+    """num_first + num_last = topk: no page is scored, so no query, mean or page of the table is looked at, and the workspace holds nothing."""
+    page, T = 16, sum(chunk)
+    most = max(p + c for p, c in zip(prefix, chunk))
+    nothing = torch.full((T, 4, 128), float("nan"), dtype=torch.bfloat16, device="cuda")
+    table = torch.full((len(prefix), -(-most // page)), -1, dtype=torch.int32, device="cuda")
+    means = torch.full((3, 2, 128), float("nan"), dtype=torch.bfloat16, device="cuda")
+    ws = torch.empty(api.vpp_block_select_workspace_size(T, len(prefix), 4, 2, page, most, topk, first, topk - first), dtype=torch.uint8, device="cuda")
+    got = torch.full((T + 1, 2, topk), -77, dtype=torch.int32, device="cuda")
+    for c, want in ((chunk, 0), ([chunk[0] + 1] + chunk[1:], 1), (chunk, 0)):
+        status = ints([-1])
+        api.vpp_block_select(nothing, means, table, ints(prefix), ints(c), page, most + 1, got[:T], ws, num_first=first, num_last=topk - first, status=status)
+        assert int(status) == want
+        if want:
+            assert (got == -77).all()
+        else:
+            lists = ref_block_select(np.zeros((T, 4, 128)), np.zeros((1, 2, 128)), np.zeros(table.shape, np.int64), prefix, c, page, topk, first, topk - first)
+            assert (got[:T].cpu().numpy() == lists).all() and (got[T] == -77).all()
+            got.fill_(-77)
