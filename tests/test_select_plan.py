@@ -50,6 +50,7 @@ def test_a_workspace_of_the_size_that_the_binding_gives_is_enough():
         want, at = needed(T, R, hq, hkv, page, most, topk, first, last), (T, R, hq, hkv, page, most)
         size = lambda *choice, **kw: api.vpp_block_select_workspace_size(*at, *choice, **kw)      # noqa: E731
         assert 0 < want == size(topk, first, last), (at, topk, first, last)
+        assert size(topk) == max(needed(*at, k, 0, 1) for k in range(1, topk + 1))
         assert want <= min(size(), size(topk), size(topk, first), size(topk, num_last=last)), (at, topk, first, last)
 
 
