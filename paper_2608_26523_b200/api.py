@@ -228,18 +228,23 @@ def _current_stream():
     return _raw_stream(_current_device())
 
 
+def _dense_table(block_table):
+    """Whether a request's row of the table begins where the last one's ends, as the library has it (a slice of a wider table does not)."""
+    return block_table is None or block_table.is_contiguous()
+
+
 def make_args(q, k_cache, v_cache, block_table, prefix_len, chunk_len, block_size, max_seq_len,
               softmax_scale, num_kv_splits=0, out=None, lse=None, workspace=None, status=None,
               total_q=None, head_dim_v=None):
     """Fill a vpp_chunk_attn_args from tensors.
 
     q [T, Hq, Dqk] bf16; k_cache/v_cache [num_blocks, block_size, Hkv, D] bf16 (any strides with a
-    contiguous last dim; v may be a view of k); block_table int32 [R, max_blocks] or None.
+    contiguous last dim; v may be a view of k); block_table int32 [R, max_blocks], dense, or None.
     """
     a = ChunkAttnArgs()
     a.q, a.k_cache, a.v_cache = _ptr(q), _ptr(k_cache), _ptr(v_cache)
     ks, vs = k_cache.stride(), v_cache.stride()
-    assert ks[3] == 1 and vs[3] == 1 and q.is_contiguous()
+    assert ks[3] == 1 and vs[3] == 1 and q.is_contiguous() and _dense_table(block_table)
     a.k_block_stride, a.k_token_stride, a.k_head_stride = ks[0], ks[1], ks[2]
     a.v_block_stride, a.v_token_stride, a.v_head_stride = vs[0], vs[1], vs[2]
     a.block_table = _ptr(block_table)
@@ -365,10 +370,10 @@ def vpp_kv_append_rope(k_new, v_new, k_cache, v_cache, block_table, prefix_len, 
                        q_out=None, layout="half", rot_offset=0, amplitude=1.0, status=None, stream=None):
     """vpp_kv_append with the keys rotated to their positions on the way, and q [T, Hq, Dqk] rotated into q_out (both or neither).
 
-    k_new, v_new, q, q_out: any strides with a contiguous last dim, as slices of a fused projection have them."""
+    k_new, v_new, q, q_out: any strides with a contiguous last dim, as slices of a fused projection have them; block_table int32 [R, max_blocks], dense, or None."""
     bf16 = torch.bfloat16
     shape, ns, ks = k_new.shape, k_new.stride(), k_cache.stride()
-    assert k_new.dtype is k_cache.dtype is bf16 and ns[2] == 1 == ks[3]
+    assert k_new.dtype is k_cache.dtype is bf16 and ns[2] == 1 == ks[3] and _dense_table(block_table)
     assert inv_freq.dtype is torch.float32 and inv_freq.is_contiguous()
     if v_new is not None:
         v_ptr, vn, vs, dim_v = v_new.data_ptr(), v_new.stride(), v_cache.stride(), v_new.shape[2]
@@ -399,7 +404,7 @@ def vpp_block_means(k_cache, k_means, block_table, prefix_len, chunk_len, block_
     contiguous last dim; k_means [num_blocks, Hkv, 128] bf16, dense."""
     ks, shape = k_cache.stride(), k_cache.shape
     assert ks[3] == 1 and k_means.is_contiguous() and k_cache.dtype is k_means.dtype is torch.bfloat16
-    assert k_means.shape == (shape[0], shape[2], shape[3])
+    assert k_means.shape == (shape[0], shape[2], shape[3]) and _dense_table(block_table)
     a = _PACK_MEANS.pack(k_cache.data_ptr(), ks[0], ks[1], ks[2], k_means.data_ptr(), 0 if block_table is None else block_table.data_ptr(),
                          prefix_len.data_ptr(), chunk_len.data_ptr(), prefix_len.numel(), 0 if block_table is None else block_table.shape[1],
                          block_size, shape[0], total_q, shape[2], shape[3], 0 if status is None else status.data_ptr())
@@ -435,7 +440,7 @@ def vpp_block_select(q, k_means, block_table, prefix_len, chunk_len, block_size,
     """indices [T, Hkv, topk] int32 <- the pages that each token's queries score highest (see include/vpp.h).  q [T, Hq, 128] bf16 dense,
     k_means [num_blocks, Hkv, 128]; workspace of vpp_block_select_workspace_size(...) bytes."""
     q_shape, i_shape = q.shape, indices.shape
-    assert q.is_contiguous() and k_means.is_contiguous() and indices.is_contiguous() and indices.dtype is torch.int32
+    assert q.is_contiguous() and k_means.is_contiguous() and indices.is_contiguous() and indices.dtype is torch.int32 and _dense_table(block_table)
     assert i_shape[0] == q_shape[0] and i_shape[1] == k_means.shape[1] and q.dtype is k_means.dtype is torch.bfloat16 and q_shape[2] == k_means.shape[2]
     a = _PACK_SELECT.pack(q.data_ptr(), k_means.data_ptr(), 0 if block_table is None else block_table.data_ptr(), prefix_len.data_ptr(),
                           chunk_len.data_ptr(), prefix_len.numel(), 0 if block_table is None else block_table.shape[1], block_size, k_means.shape[0], q_shape[0],
