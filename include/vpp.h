@@ -515,6 +515,9 @@ vpp_status vpp_block_means(const vpp_block_means_args *args, vpp_stream_t stream
  * Candidates are kept for up to 128 MiB worth of tokens at a time, or for 256 tokens where those take more (hundreds of kv-heads; dozens of them with more than 32
  * of tens of thousands of pages to pick; millions of pages): the workspace grows no further with the chunk.  Past 4 GiB VPP_ERR_UNSUPPORTED.  Its size is not
  * monotone in topk, num_first, num_last or total_q (fewer may need more): ask for every combination that the calls of one workspace have.
+ * Cost: the queries once and two products a page.  Where 32 bits cannot tell -- an infinite or NaN mean among a token's scored pages (or those of up to 255 neighbours), more than
+ * a hundred or so pages within rounding of the last one listed, as zero or repeated keys have them -- all its pages are scored in 64 bits, at forty to sixty times the time (8192
+ * tokens of 64/4 heads, 1152 pages: 125 us, then 5.6 to 7.1 ms).
  * Returns after enqueueing two or three kernels on `stream` for each of those portions of the tokens (one kernel where num_first + num_last = topk: no page is scored).
  */
 typedef struct {

@@ -13,7 +13,7 @@
 // own with an accumulator of its own.  Scores have two buffers in tensor memory (S 128 columns | S 128 | O_0 | O_1), so that the groups work on
 // one step's while the tensor core runs P V of the last and forms the next.  The scores of both groups are one MMA chain of 128 keys, and a step has two commits: "scores"
 // (also: the K stage and Q are free) and "P V" (also: the V stage is free, O is quiet).  4096 tokens of 64/4 heads, lists of
-// 32 pages of 64, unions of 68, 34 steps a tile: 558 us, 1040 TFLOP/s over the unions (930 at the power limit).  Tried before:
+// 32 pages of 64, unions of 68, 34 steps a tile: 557 us in a captured graph, 1048 TFLOP/s over the unions; as calls one after the other, at the power limit, 648 us, 900.  Tried before:
 // whole steps in turn, one buffer a group, 690 us (a group waits 1900 clk for its next scores); a chain of 64 keys and commits of its own for each
 // group, 690 us (2500 clk a step, 1800 of them the issue of 24 MMAs and 4 commits).  At the end both join the two results, half the features
 // each.  Q has two buffers, so that the next item's first scores are formed under the join.
@@ -21,6 +21,8 @@
 // and the maxima of 16 columns, not to every score; the own page, which is seen in part, goes through the scores.
 //   warp 0      scheduler, K producer      warp 1  the thread that issues the MMAs
 //   warp 2      V producer, tensor memory  warps 4-7, 8-11  softmax groups
+// Scores, maxima, sums and accumulators are in 32 bits; the weights are rounded to bf16, half a step of 2^-8 each, because the tensor core takes both operands of P V in one type and
+// V is bf16 (two parts of a weight would double that product).  The result's error against 64 bits is 2.3e-3 (relative 2-norm), of which its own rounding is 1.7e-3.
 // Every wait is bounded, as in attn_ws.cuh, whose lazy rescale and packed fma this kernel has too.
 // (A quarter of the exponentials as polynomials by fused multiply-adds: 551 -> 560 us; half: 592.)
 #pragma once

@@ -4,7 +4,8 @@
 // its keys are in the cache.  One work item is (completed page, kv-head): block_size rows of 256 bytes, read once -- HBM-bound.  16 lanes
 // a key, a lane per 16-byte vector, up to kMeansUnroll loads in flight a lane, and the next item's page looked up under them.  Items of up to 64 keys are
 // a warp's, longer ones a block's (which adds its eight groups' sums in shared memory).  Sums are in 32 bits, in one fixed order; the mean is rounded once, to bf16.
-// A context of 131072 tokens and 8 kv-heads, pages of 64 / 16: 45.5 / 51.8 us, 5.9 / 5.2 TB/s (a block an item: 66 / 217 us); 16384 keys in pages of 128, 8.1 us, 4.1 TB/s.
+// A context of 131072 tokens and 8 kv-heads, pages of 64 / 16: 45.5 / 51.8 us, 5.9 / 5.2 TB/s (a block an item: 66 / 217 us); 16384 keys in pages of 128, 8.2 us, 4.1 TB/s (all in a
+// captured graph; as calls one after the other the last takes 9.7).
 #pragma once
 #include <cstdint>
 

@@ -18,8 +18,10 @@
 //  * block_few_kernel: tokens of requests of up to kSelectFew in the slab -- decode rows, a last rest -- multiplied by warps from the registers that the loads fill, the scores in
 //    shared memory: there reading the means is all.
 //  * block_pick_kernel: a warp a (token, kv-head) ranks the candidates and settles the border.
-// 8192 tokens of 64/4 heads, 1152 pages, lists of 32: 124 us, of which the filter takes 88: 26 reading 134 MB of q (21 at the copy rate), then 18 steps of 2.4 (maxima)
+// 8192 tokens of 64/4 heads, 1152 pages, lists of 32: 125 us in a captured graph (132 as calls one after the other), of which the filter takes 88: 26 reading 134 MB of q (21 at the copy rate), then 18 steps of 2.4 (maxima)
 // and 4.4 thousand clk (lists), where the products take 2.05; of its issue slots 48 %, of the tensor pipe 24 %.  One row of twenty has pages too close for 32 bits (8 us).
+// An infinite or NaN mean, or more than `cap` pages of one half within the bound of the border (zero or repeated keys), send every row that scores them through 64 bits, a page after the other
+// (pick_thorough): the same call takes 5.6 to 7.1 ms then, 16 decode rows 0.15 to 1.0 ms instead of 27 us.
 // Before: all scores written down once, 4.6 KB a token and kv-head, and picked from there, 420 us; items of 128 tokens, eight warps that do one thing after the
 // other, two an SM, 195; items of 224 tokens, 148 of them, 130; means fetched and bounded by the four other warps alone, 3900 clk a step for 64 copies.
 #pragma once

@@ -9,8 +9,8 @@
 // kind (queries, keys or values) at a time, kRopeUnroll units a lane, a unit being two 16-byte vectors of one head that hold each other's
 // partners ("half": vectors u and u + rot_dim / 16).  Its loads are issued first; while they are in flight the warp looks up the token's
 // request, position and page and works out the token's cosines and sines, once for all heads of the piece (two angles a lane at 128 rotated
-// features), in 512 bytes of shared memory of its own.  16384 tokens of 64/8 heads: 112.7 us, 5.96 TB/s, 91 % of the copy rate; 8192 tokens of 128 x 64
-// features into wider rows 46.3 us (89 %).  Tried: pieces that mix the kinds, with a division for each unit (1160 instructions a piece, 69 % of the issue
+// features), in 512 bytes of shared memory of its own.  16384 tokens of 64/8 heads: 112 us in a captured graph, 6.0 TB/s, 92 % of the copy rate (as calls one after the other 121, 85 %); 8192 tokens of
+// 128 x 64 features into wider rows 46.3 us, 89 % (48.6).  Tried: pieces that mix the kinds, with a division for each unit (1160 instructions a piece, 69 % of the issue
 // slots: 119 and 52 us); pieces of two and four rounds with one set of angles (146 and 129 us, 46.3 both); 32 warps an SM instead of 24 (114 and 51 us).
 //
 // Angles: pos * inv_freq is formed in 64 bits and reduced to half a turn there (32 bits are off by 0.03 rad at a position of a million), the
